@@ -13,6 +13,8 @@ _EXPORTS = {
     "maxpool2d_f32", "maxpool2d_out_dims", "maxpool2d", "Net", "Layer",
     "conv2d_fwd_f32_workspace_bytes", "conv2d_fwd_f32_plan_string",
     "conv2d_fwd_f32_plan_info", "mg3m_padding_overhead", "mg3m_time_next_kernel", "mg3m_status_string",
+    "conv1d_causal", "conv1d_causal_step", "selective_scan", "selective_scan_step",
+    "selective_scan_workspace_bytes", "matvec_w4",
     "mg3m_last_error", "load_library", "Mg3mError", "HWCN", "NCHW",
 }
 

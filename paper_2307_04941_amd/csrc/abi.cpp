@@ -19,6 +19,7 @@
 
 #include "mg3m.h"
 #include "mg3m_internal.h"
+#include "seq.h"
 
 namespace {
 
@@ -431,6 +432,28 @@ namespace mg3m {
 
 int set_error(int status, const std::string& msg) { return fail(status, msg); }
 void clear_error() { g_last_error.clear(); }
+
+int take_workspace(void* stream, size_t bytes, CallWorkspace* w, std::string* err) {
+  float* p = nullptr;
+  hipEvent_t done = nullptr;
+  const int rc = own_workspace_for(stream, bytes, &p, &done, &w->lock, err);
+  w->ptr = p;
+  w->done = done;
+  return rc;
+}
+
+int give_workspace(void* stream, CallWorkspace* w, int rc, std::string* err) {
+  hipStream_t st = static_cast<hipStream_t>(stream);
+  // recorded even after a failed launch: a later call waits for what was queued
+  const bool kept = w->done != nullptr;
+  const hipError_t e = kept ? hipEventRecord(static_cast<hipEvent_t>(w->done), st) : hipFreeAsync(w->ptr, st);
+  if (w->lock.owns_lock()) w->lock.unlock();
+  if (rc == MG3M_OK && e != hipSuccess) {
+    *err = std::string(kept ? "hipEventRecord: " : "hipFreeAsync: ") + hipGetErrorString(e);
+    return MG3M_ERR_HIP;
+  }
+  return rc;
+}
 
 int conv_run(const float* x, const float* w, float* y, const ConvGeom& g, void* workspace,
              size_t workspace_bytes, bool own_workspace, const char* plan, const float* add, int relu,

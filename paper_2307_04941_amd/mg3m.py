@@ -1,4 +1,5 @@
-"""Thin Python binding of the C ABI in include/mg3m.h (libmg3m.so).
+"""Thin Python binding of the C ABI in include/mg3m.h and include/mg3m_seq.h
+(libmg3m.so).
 
 Functions carry the C names and only marshal arguments: every step of the
 convolution runs in the library's HIP kernels.  Device buffers are torch
@@ -10,6 +11,7 @@ from __future__ import annotations
 
 import ctypes
 import os
+import struct
 from typing import Optional
 
 _PKG = os.path.dirname(os.path.abspath(__file__))
@@ -122,6 +124,12 @@ def load_library(path: str = LIB_PATH):
     lib.mg3m_last_error.argtypes = []
     lib.mg3m_last_error.restype = ctypes.c_char_p
     lib.mg3m_trim_workspace_pool.argtypes = []
+    for name in ("conv1d_causal_fwd", "conv1d_causal_step", "selective_scan_fwd", "selective_scan_step",
+                 "matvec_w4_fwd"):
+        getattr(lib, name).argtypes = [ctypes.c_char_p, p]
+        getattr(lib, name).restype = i
+    lib.selective_scan_workspace_bytes.argtypes = [i] * 5 + [ctypes.POINTER(sz)]
+    lib.selective_scan_workspace_bytes.restype = i
     for name in ("conv2d_out_dims", "conv2d_out_dims_hw", "conv2d_fwd_f32_hw",
                  "conv2d_fwd_f32_hw_workspace_bytes", "conv2d_fwd_f32_acc64",
                  "conv2d_fwd_f32_acc64_plan_string", "conv2d_fwd_f32_fused", "maxpool2d_f32",
@@ -521,4 +529,225 @@ def conv2d_fwd(x, w, stride=1, pad=0, layout="HWCN", plan: Optional[str] = None,
     else:
         conv2d_fwd_f32_hw(x, w, y, N, C, H, W, K, R, S, sh, sw, ph, pw, layout, workspace, wsz,
                           plan, stream)
+    return y
+
+
+# -------------------------------------------------------- sequence operators
+# The argument structs of include/mg3m_seq.h, in its order.
+_CONV1D = struct.Struct("7P2q4i4i")
+_SCAN = struct.Struct("13PN6q5i3i")
+_W4 = struct.Struct("5P2q6i")
+
+
+def _dtype_code(t) -> int:
+    import torch
+    code = {torch.float32: 0, torch.bfloat16: 1, torch.float16: 2}.get(t.dtype)
+    if code is None:
+        raise TypeError(f"tensor must be float32, bfloat16 or float16, not {t.dtype}")
+    return code
+
+
+def _rows_of(t, name, like=None, tail=1):
+    """(address, distance between rows in elements) of a tensor of rows: its
+    last `tail` sizes are a row, dense; the leading ones count rows that lie
+    at one distance."""
+    if not t.is_cuda:
+        raise ValueError(f"{name} must live on the GPU")
+    if like is not None:
+        if t.dtype != like.dtype:
+            raise TypeError(f"{name} must be {like.dtype}, not {t.dtype}")
+        if t.device != like.device:
+            raise ValueError(f"{name} is on {t.device}, not {like.device}")
+    shape = t.shape
+    cols = 1
+    for v in shape[len(shape) - tail:]:
+        cols *= v
+    if t.is_contiguous():
+        return t.data_ptr(), cols
+    strides, width = t.stride(), 1
+    for i in range(len(shape) - 1, len(shape) - 1 - tail, -1):
+        if shape[i] != 1 and strides[i] != width:
+            raise ValueError(f"the channels of {name} must be contiguous")
+        width *= shape[i]
+    ld = None
+    for i in range(len(shape) - tail - 1, -1, -1):
+        if shape[i] == 1:
+            continue
+        if ld is None:
+            ld, rows = strides[i], shape[i]
+        elif strides[i] != ld * rows:
+            raise ValueError(f"the rows of {name} must lie at one distance")
+        else:
+            rows *= shape[i]
+    return t.data_ptr(), cols if ld is None else ld
+
+
+def _dense_of(t, name, shape, dtype, device) -> int:
+    if t is None:
+        return 0
+    if t.dtype != dtype:
+        raise TypeError(f"{name} must be {dtype}, not {t.dtype}")
+    if t.device != device:
+        raise ValueError(f"{name} is on {t.device}, not {device}")
+    if tuple(t.shape) != shape:
+        raise ValueError(f"{name} has shape {tuple(t.shape)}, expected {shape}")
+    if not t.is_contiguous():
+        raise ValueError(f"{name} must be contiguous")
+    return t.data_ptr()
+
+
+def _on_current(t):
+    import torch
+    if not t.is_cuda:
+        raise ValueError("tensor must live on the GPU")
+    if t.device.index != torch.cuda.current_device():
+        raise ValueError(f"tensors are on {t.device}, which is not the current device")
+
+
+def _like_rows(out, lead, name, like):
+    import torch
+    if out is None:
+        return torch.empty(lead, dtype=like.dtype, device=like.device)
+    if tuple(out.shape) != tuple(lead):
+        raise ValueError(f"{name} has shape {tuple(out.shape)}, expected {tuple(lead)}")
+    return out
+
+
+def _sequences(x, offsets, begin, end):
+    """(rows, sequences, begin address, end address) of a call whose row
+    tensor is x: (T, channels), or (N, L, channels) for N equal sequences."""
+    import torch
+    if x.dim() not in (2, 3):
+        raise ValueError("rows come as (T, channels) or (N, L, channels)")
+    T = x.shape[0] if x.dim() == 2 else x.shape[0] * x.shape[1]
+    if offsets is None and begin is None and end is None:
+        return T, (1 if x.dim() == 2 else x.shape[0]), 0, 0
+    if offsets is not None:
+        if begin is not None or end is not None:
+            raise ValueError("give offsets, or begin and end")
+        n = offsets.shape[0] - 1
+        at = _dense_of(offsets, "offsets", (n + 1,), torch.int32, x.device)
+        return T, n, at, at + 4
+    if begin is None or end is None:
+        raise ValueError("give begin and end, or neither")
+    n = begin.shape[0]
+    return (T, n, _dense_of(begin, "begin", (n,), torch.int32, x.device),
+            _dense_of(end, "end", (n,), torch.int32, x.device))
+
+
+def conv1d_causal(x, w, bias=None, silu=False, state=None, load_state=False, offsets=None, begin=None, end=None,
+                  out=None, stream=None):
+    """Causal depthwise convolution along tokens (conv1d_causal_fwd).
+
+    x: (N, L, C) for N equal sequences, or (T, C): one sequence, or with
+    offsets (N + 1) or begin and end (N each; int32, on the GPU) the rows of N
+    sequences.  w: (R, C); bias: (C); state: (N, R - 1, C), written in place
+    and with load_state read first.  Returns y, shaped as x."""
+    _on_current(x)
+    T, n, b, e = _sequences(x, offsets, begin, end)
+    C, R = x.shape[-1], w.shape[0]
+    y = _like_rows(out, x.shape, "out", x)
+    xp, ldx = _rows_of(x, "x")
+    yp, ldy = _rows_of(y, "out", x)
+    a = _CONV1D.pack(xp, _dense_of(w, "w", (R, C), x.dtype, x.device), _dense_of(bias, "bias", (C,), x.dtype, x.device),
+                     _dense_of(state, "state", (n, R - 1, C), x.dtype, x.device), yp, b, e, ldx, ldy, T, C, R, n,
+                     int(load_state), int(silu), _dtype_code(x), 0)
+    _check(load_library().conv1d_causal_fwd(a, _stream(stream)))
+    return y
+
+
+def conv1d_causal_step(x, w, state, bias=None, silu=False, out=None, stream=None):
+    """One token of each of N sequences (conv1d_causal_step): x (N, C), state
+    (N, R - 1, C) read and shifted in place (None if R = 1)."""
+    _on_current(x)
+    (n, C), R = x.shape, w.shape[0]
+    y = _like_rows(out, x.shape, "out", x)
+    xp, ldx = _rows_of(x, "x")
+    yp, ldy = _rows_of(y, "out", x)
+    a = _CONV1D.pack(xp, _dense_of(w, "w", (R, C), x.dtype, x.device), _dense_of(bias, "bias", (C,), x.dtype, x.device),
+                     _dense_of(state, "state", (n, R - 1, C), x.dtype, x.device), yp, 0, 0, ldx, ldy, n, C, R, n, 1,
+                     int(silu), _dtype_code(x), 0)
+    _check(load_library().conv1d_causal_step(a, _stream(stream)))
+    return y
+
+
+def selective_scan_workspace_bytes(T, D, G, S, N) -> int:
+    b = ctypes.c_size_t()
+    _check(load_library().selective_scan_workspace_bytes(T, D, G, S, N, ctypes.byref(b)))
+    return b.value
+
+
+def _scan_args(u, dt, A, B, C, D, z, dt_bias, softplus, state, load_state, T, n, begin, end, workspace, out):
+    import torch
+    if B.dim() not in (u.dim(), u.dim() + 1):
+        raise ValueError("B is rows of S values, or of (G, S)")
+    Dn, S, tail = u.shape[-1], B.shape[-1], B.dim() - u.dim() + 1
+    G = B.shape[-2] if tail == 2 else 1
+    dev, f32 = u.device, torch.float32
+    for t, name, shape in ((dt, "dt", u.shape), (z, "z", u.shape), (B, "B", (*u.shape[:-1], *B.shape[B.dim() - tail:])),
+                           (C, "C", B.shape)):
+        if t is not None and tuple(t.shape) != tuple(shape):
+            raise ValueError(f"{name} has shape {tuple(t.shape)}, expected {tuple(shape)}")
+    (up, ldu), (dp, lddt) = _rows_of(u, "u"), _rows_of(dt, "dt", u)
+    (bp, ldb), (cp, ldc) = _rows_of(B, "B", u, tail), _rows_of(C, "C", u, tail)
+    zp, ldz = (0, Dn) if z is None else _rows_of(z, "z", u)
+    y = _like_rows(out, u.shape, "out", u)
+    yp, ldy = _rows_of(y, "out", u)
+    wp = 0 if workspace is None else workspace.data_ptr()
+    wb = 0 if workspace is None else workspace.numel() * workspace.element_size()
+    return y, _SCAN.pack(up, dp, _dense_of(A, "A", (Dn, S), f32, dev), bp, cp, _dense_of(D, "D", (Dn,), f32, dev), zp,
+                         _dense_of(dt_bias, "dt_bias", (Dn,), f32, dev), _dense_of(state, "state", (n, Dn, S), f32, dev),
+                         yp, begin, end, wp, wb, ldu, lddt, ldb, ldc, ldz, ldy, T, Dn, G, S, n, int(load_state),
+                         int(softplus), _dtype_code(u))
+
+
+def selective_scan(u, dt, A, B, C, D=None, z=None, dt_bias=None, softplus=False, state=None, load_state=False,
+                   offsets=None, begin=None, end=None, workspace=None, out=None, stream=None):
+    """Selective state space scan (selective_scan_fwd).
+
+    u, dt, z: rows of D channels, (N, L, D) or (T, D), the sequences as in
+    conv1d_causal.  B, C: rows of (G, S), or of S values for one group.  A:
+    (D, S), D and dt_bias: (D), state: (N, D, S), all float32; state is written
+    in place and with load_state read first.  workspace: a tensor of at least
+    selective_scan_workspace_bytes(), or None for the library's own.  Returns
+    y, shaped as u."""
+    _on_current(u)
+    T, n, b, e = _sequences(u, offsets, begin, end)
+    y, a = _scan_args(u, dt, A, B, C, D, z, dt_bias, softplus, state, load_state, T, n, b, e, workspace, out)
+    _check(load_library().selective_scan_fwd(a, _stream(stream)))
+    return y
+
+
+def selective_scan_step(u, dt, A, B, C, state, D=None, z=None, dt_bias=None, softplus=False, out=None, stream=None):
+    """One token of each of N sequences (selective_scan_step): u, dt, z (N, D),
+    B, C (N, G, S) or (N, S), state (N, D, S) read and updated in place."""
+    _on_current(u)
+    n = u.shape[0]
+    y, a = _scan_args(u, dt, A, B, C, D, z, dt_bias, softplus, state, True, n, n, 0, 0, None, out)
+    _check(load_library().selective_scan_step(a, _stream(stream)))
+    return y
+
+
+def matvec_w4(x, q, scale, zero=None, out=None, stream=None):
+    """Product of M tokens with 4-bit weights (matvec_w4_fwd): x (M, C) or
+    (C,), q (K, C / 2) uint8 with the even channel in the low four bits, scale
+    (K, C / group) of x's type, zero the same shape in uint8 (None: 8).
+    Returns (M, K) or (K,)."""
+    import torch
+    _on_current(x)
+    if x.dim() not in (1, 2):
+        raise ValueError("x is (M, C) or (C,)")
+    C, K = x.shape[-1], q.shape[0]
+    M = 1 if x.dim() == 1 else x.shape[0]
+    groups = scale.shape[-1]
+    if groups < 1 or C % groups:
+        raise ValueError(f"{groups} groups do not divide {C} channels")
+    y = _like_rows(out, (K,) if x.dim() == 1 else (M, K), "out", x)
+    xp, ldx = _rows_of(x, "x")
+    yp, ldy = _rows_of(y, "out", x)
+    dev = x.device
+    a = _W4.pack(xp, _dense_of(q, "q", (K, C // 2), torch.uint8, dev), _dense_of(scale, "scale", (K, groups), x.dtype, dev),
+                 _dense_of(zero, "zero", (K, groups), torch.uint8, dev), yp, ldx, ldy, M, C, K, C // groups,
+                 _dtype_code(x), 0)
+    _check(load_library().matvec_w4_fwd(a, _stream(stream)))
     return y
