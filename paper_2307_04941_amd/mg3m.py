@@ -539,32 +539,53 @@ _SCAN = struct.Struct("13PN6q5i3i")
 _W4 = struct.Struct("5P2q6i")
 
 
-def _dtype_code(t) -> int:
+# The smallest calls take less time on the device than in this binding, so it
+# looks at each tensor once and builds no torch objects that it can do without
+# (a Stream object, a shape tuple, a device).  torch is imported on first use.
+_torch = None
+_DTYPES = {}
+_raw_stream = None
+
+
+def _seq_torch():
+    global _torch, _raw_stream
     import torch
-    code = {torch.float32: 0, torch.bfloat16: 1, torch.float16: 2}.get(t.dtype)
+    _DTYPES.update({torch.float32: 0, torch.bfloat16: 1, torch.float16: 2})
+    _raw_stream = getattr(torch._C, "_cuda_getCurrentRawStream", None) or (
+        lambda dev: torch.cuda.current_stream(dev).cuda_stream)
+    _torch = torch
+    return torch
+
+
+def _seq_call(fn, packed, dev, stream):
+    if stream is None:
+        stream = _raw_stream(dev)
+    elif not isinstance(stream, int):
+        stream = stream.cuda_stream
+    rc = getattr(_lib or load_library(), fn)(packed, stream)
+    if rc:
+        raise Mg3mError(rc, mg3m_last_error())
+
+
+def _first(t):
+    """(device, dtype, its code) of a call, from its first tensor."""
+    torch = _torch or _seq_torch()
+    dev, dtype = t.get_device(), t.dtype
+    if dev < 0:
+        raise ValueError("tensor must live on the GPU")
+    if dev != torch.cuda.current_device():
+        raise ValueError(f"tensors are on cuda:{dev}, which is not the current device")
+    code = _DTYPES.get(dtype)
     if code is None:
-        raise TypeError(f"tensor must be float32, bfloat16 or float16, not {t.dtype}")
-    return code
+        raise TypeError(f"tensor must be float32, bfloat16 or float16, not {dtype}")
+    return dev, dtype, code
 
 
-def _rows_of(t, name, like=None, tail=1):
-    """(address, distance between rows in elements) of a tensor of rows: its
-    last `tail` sizes are a row, dense; the leading ones count rows that lie
-    at one distance."""
-    if not t.is_cuda:
-        raise ValueError(f"{name} must live on the GPU")
-    if like is not None:
-        if t.dtype != like.dtype:
-            raise TypeError(f"{name} must be {like.dtype}, not {t.dtype}")
-        if t.device != like.device:
-            raise ValueError(f"{name} is on {t.device}, not {like.device}")
-    shape = t.shape
-    cols = 1
-    for v in shape[len(shape) - tail:]:
-        cols *= v
-    if t.is_contiguous():
-        return t.data_ptr(), cols
-    strides, width = t.stride(), 1
+def _row_distance(t, name, tail=1):
+    """The distance between rows, in elements, of a tensor of rows: its last
+    `tail` sizes are a row, dense; the leading ones count rows that lie at one
+    distance."""
+    shape, strides, width = t.shape, t.stride(), 1
     for i in range(len(shape) - 1, len(shape) - 1 - tail, -1):
         if shape[i] != 1 and strides[i] != width:
             raise ValueError(f"the channels of {name} must be contiguous")
@@ -579,44 +600,48 @@ def _rows_of(t, name, like=None, tail=1):
             raise ValueError(f"the rows of {name} must lie at one distance")
         else:
             rows *= shape[i]
-    return t.data_ptr(), cols if ld is None else ld
+    return width if ld is None else ld
 
 
-def _dense_of(t, name, shape, dtype, device) -> int:
+def _rows_of(t, name, shape, dtype, dev, tail=1):
+    """(address, distance between rows) of a tensor of rows of this shape."""
+    if t.dtype is not dtype or t.get_device() != dev or t.shape != shape:
+        _refuse(t, name, shape, dtype, dev)
+    if t.is_contiguous():
+        return t.data_ptr(), (shape[-1] if tail == 1 else shape[-1] * shape[-2])
+    return t.data_ptr(), _row_distance(t, name, tail)
+
+
+def _dense_of(t, name, shape, dtype, dev) -> int:
     if t is None:
         return 0
-    if t.dtype != dtype:
-        raise TypeError(f"{name} must be {dtype}, not {t.dtype}")
-    if t.device != device:
-        raise ValueError(f"{name} is on {t.device}, not {device}")
-    if tuple(t.shape) != shape:
-        raise ValueError(f"{name} has shape {tuple(t.shape)}, expected {shape}")
+    if t.dtype is not dtype or t.get_device() != dev or t.shape != shape:
+        _refuse(t, name, shape, dtype, dev)
     if not t.is_contiguous():
         raise ValueError(f"{name} must be contiguous")
     return t.data_ptr()
 
 
-def _on_current(t):
-    import torch
-    if not t.is_cuda:
-        raise ValueError("tensor must live on the GPU")
-    if t.device.index != torch.cuda.current_device():
-        raise ValueError(f"tensors are on {t.device}, which is not the current device")
+def _refuse(t, name, shape, dtype, dev):
+    if t.dtype is not dtype:
+        raise TypeError(f"{name} must be {dtype}, not {t.dtype}")
+    if t.get_device() != dev:
+        raise ValueError(f"{name} is on {t.device}, not cuda:{dev}")
+    raise ValueError(f"{name} has shape {tuple(t.shape)}, expected {tuple(shape)}")
 
 
-def _like_rows(out, lead, name, like):
-    import torch
+def _out_rows(out, shape, like, dtype, dev):
+    """(result, its address, its distance between rows)."""
     if out is None:
-        return torch.empty(lead, dtype=like.dtype, device=like.device)
-    if tuple(out.shape) != tuple(lead):
-        raise ValueError(f"{name} has shape {tuple(out.shape)}, expected {tuple(lead)}")
-    return out
+        out = like.new_empty(shape)
+        return out, out.data_ptr(), shape[-1]
+    p, ld = _rows_of(out, "out", shape, dtype, dev)
+    return out, p, ld
 
 
-def _sequences(x, offsets, begin, end):
+def _sequences(x, dev, offsets, begin, end):
     """(rows, sequences, begin address, end address) of a call whose row
     tensor is x: (T, channels), or (N, L, channels) for N equal sequences."""
-    import torch
     if x.dim() not in (2, 3):
         raise ValueError("rows come as (T, channels) or (N, L, channels)")
     T = x.shape[0] if x.dim() == 2 else x.shape[0] * x.shape[1]
@@ -626,13 +651,23 @@ def _sequences(x, offsets, begin, end):
         if begin is not None or end is not None:
             raise ValueError("give offsets, or begin and end")
         n = offsets.shape[0] - 1
-        at = _dense_of(offsets, "offsets", (n + 1,), torch.int32, x.device)
+        at = _dense_of(offsets, "offsets", (n + 1,), _torch.int32, dev)
         return T, n, at, at + 4
     if begin is None or end is None:
         raise ValueError("give begin and end, or neither")
     n = begin.shape[0]
-    return (T, n, _dense_of(begin, "begin", (n,), torch.int32, x.device),
-            _dense_of(end, "end", (n,), torch.int32, x.device))
+    return (T, n, _dense_of(begin, "begin", (n,), _torch.int32, dev), _dense_of(end, "end", (n,), _torch.int32, dev))
+
+
+def _conv1d(fn, x, w, bias, silu, state, load, dev, dtype, code, T, n, begin, end, out, stream):
+    shape, R = x.shape, w.shape[0]
+    C = shape[-1]
+    xp, ldx = _rows_of(x, "x", shape, dtype, dev)
+    out, yp, ldy = _out_rows(out, shape, x, dtype, dev)
+    _seq_call(fn, _CONV1D.pack(xp, _dense_of(w, "w", (R, C), dtype, dev), _dense_of(bias, "bias", (C,), dtype, dev),
+                               _dense_of(state, "state", (n, R - 1, C), dtype, dev), yp, begin, end, ldx, ldy, T, C, R,
+                               n, 1 if load else 0, 1 if silu else 0, code, 0), dev, stream)
+    return out
 
 
 def conv1d_causal(x, w, bias=None, silu=False, state=None, load_state=False, offsets=None, begin=None, end=None,
@@ -643,32 +678,19 @@ def conv1d_causal(x, w, bias=None, silu=False, state=None, load_state=False, off
     offsets (N + 1) or begin and end (N each; int32, on the GPU) the rows of N
     sequences.  w: (R, C); bias: (C); state: (N, R - 1, C), written in place
     and with load_state read first.  Returns y, shaped as x."""
-    _on_current(x)
-    T, n, b, e = _sequences(x, offsets, begin, end)
-    C, R = x.shape[-1], w.shape[0]
-    y = _like_rows(out, x.shape, "out", x)
-    xp, ldx = _rows_of(x, "x")
-    yp, ldy = _rows_of(y, "out", x)
-    a = _CONV1D.pack(xp, _dense_of(w, "w", (R, C), x.dtype, x.device), _dense_of(bias, "bias", (C,), x.dtype, x.device),
-                     _dense_of(state, "state", (n, R - 1, C), x.dtype, x.device), yp, b, e, ldx, ldy, T, C, R, n,
-                     int(load_state), int(silu), _dtype_code(x), 0)
-    _check(load_library().conv1d_causal_fwd(a, _stream(stream)))
-    return y
+    dev, dtype, code = _first(x)
+    T, n, b, e = _sequences(x, dev, offsets, begin, end)
+    return _conv1d("conv1d_causal_fwd", x, w, bias, silu, state, load_state, dev, dtype, code, T, n, b, e, out, stream)
 
 
 def conv1d_causal_step(x, w, state, bias=None, silu=False, out=None, stream=None):
     """One token of each of N sequences (conv1d_causal_step): x (N, C), state
     (N, R - 1, C) read and shifted in place (None if R = 1)."""
-    _on_current(x)
-    (n, C), R = x.shape, w.shape[0]
-    y = _like_rows(out, x.shape, "out", x)
-    xp, ldx = _rows_of(x, "x")
-    yp, ldy = _rows_of(y, "out", x)
-    a = _CONV1D.pack(xp, _dense_of(w, "w", (R, C), x.dtype, x.device), _dense_of(bias, "bias", (C,), x.dtype, x.device),
-                     _dense_of(state, "state", (n, R - 1, C), x.dtype, x.device), yp, 0, 0, ldx, ldy, n, C, R, n, 1,
-                     int(silu), _dtype_code(x), 0)
-    _check(load_library().conv1d_causal_step(a, _stream(stream)))
-    return y
+    dev, dtype, code = _first(x)
+    if x.dim() != 2:
+        raise ValueError("x is (N, C)")
+    n = x.shape[0]
+    return _conv1d("conv1d_causal_step", x, w, bias, silu, state, True, dev, dtype, code, n, n, 0, 0, out, stream)
 
 
 def selective_scan_workspace_bytes(T, D, G, S, N) -> int:
@@ -677,28 +699,29 @@ def selective_scan_workspace_bytes(T, D, G, S, N) -> int:
     return b.value
 
 
-def _scan_args(u, dt, A, B, C, D, z, dt_bias, softplus, state, load_state, T, n, begin, end, workspace, out):
-    import torch
-    if B.dim() not in (u.dim(), u.dim() + 1):
-        raise ValueError("B is rows of S values, or of (G, S)")
-    Dn, S, tail = u.shape[-1], B.shape[-1], B.dim() - u.dim() + 1
-    G = B.shape[-2] if tail == 2 else 1
-    dev, f32 = u.device, torch.float32
-    for t, name, shape in ((dt, "dt", u.shape), (z, "z", u.shape), (B, "B", (*u.shape[:-1], *B.shape[B.dim() - tail:])),
-                           (C, "C", B.shape)):
-        if t is not None and tuple(t.shape) != tuple(shape):
-            raise ValueError(f"{name} has shape {tuple(t.shape)}, expected {tuple(shape)}")
-    (up, ldu), (dp, lddt) = _rows_of(u, "u"), _rows_of(dt, "dt", u)
-    (bp, ldb), (cp, ldc) = _rows_of(B, "B", u, tail), _rows_of(C, "C", u, tail)
-    zp, ldz = (0, Dn) if z is None else _rows_of(z, "z", u)
-    y = _like_rows(out, u.shape, "out", u)
-    yp, ldy = _rows_of(y, "out", u)
-    wp = 0 if workspace is None else workspace.data_ptr()
-    wb = 0 if workspace is None else workspace.numel() * workspace.element_size()
-    return y, _SCAN.pack(up, dp, _dense_of(A, "A", (Dn, S), f32, dev), bp, cp, _dense_of(D, "D", (Dn,), f32, dev), zp,
-                         _dense_of(dt_bias, "dt_bias", (Dn,), f32, dev), _dense_of(state, "state", (n, Dn, S), f32, dev),
-                         yp, begin, end, wp, wb, ldu, lddt, ldb, ldc, ldz, ldy, T, Dn, G, S, n, int(load_state),
-                         int(softplus), _dtype_code(u))
+def _scan(fn, u, dt, A, B, C, D, z, dt_bias, softplus, state, load, dev, dtype, code, T, n, begin, end, workspace, out,
+          stream):
+    shape, bshape, f32 = u.shape, B.shape, _torch.float32
+    Dn, S, tail = shape[-1], bshape[-1], len(bshape) - len(shape) + 1
+    if tail not in (1, 2) or bshape[:-tail] != shape[:-1]:
+        raise ValueError(f"B has shape {tuple(bshape)}: rows like u's {tuple(shape)}, of S values or of (G, S), expected")
+    up, ldu = _rows_of(u, "u", shape, dtype, dev)
+    dp, lddt = _rows_of(dt, "dt", shape, dtype, dev)
+    bp, ldb = _rows_of(B, "B", bshape, dtype, dev, tail)
+    cp, ldc = _rows_of(C, "C", bshape, dtype, dev, tail)
+    zp, ldz = (0, Dn) if z is None else _rows_of(z, "z", shape, dtype, dev)
+    wp = wb = 0
+    if workspace is not None:
+        wp, wb = workspace.data_ptr(), workspace.numel() * workspace.element_size()
+        if workspace.get_device() != dev or not workspace.is_contiguous():
+            raise ValueError("workspace must be contiguous, on the device of the other tensors")
+    out, yp, ldy = _out_rows(out, shape, u, dtype, dev)
+    _seq_call(fn, _SCAN.pack(up, dp, _dense_of(A, "A", (Dn, S), f32, dev), bp, cp, _dense_of(D, "D", (Dn,), f32, dev),
+                             zp, _dense_of(dt_bias, "dt_bias", (Dn,), f32, dev),
+                             _dense_of(state, "state", (n, Dn, S), f32, dev), yp, begin, end, wp, wb, ldu, lddt, ldb,
+                             ldc, ldz, ldy, T, Dn, bshape[-2] if tail == 2 else 1, S, n, 1 if load else 0,
+                             1 if softplus else 0, code), dev, stream)
+    return out
 
 
 def selective_scan(u, dt, A, B, C, D=None, z=None, dt_bias=None, softplus=False, state=None, load_state=False,
@@ -711,21 +734,21 @@ def selective_scan(u, dt, A, B, C, D=None, z=None, dt_bias=None, softplus=False,
     in place and with load_state read first.  workspace: a tensor of at least
     selective_scan_workspace_bytes(), or None for the library's own.  Returns
     y, shaped as u."""
-    _on_current(u)
-    T, n, b, e = _sequences(u, offsets, begin, end)
-    y, a = _scan_args(u, dt, A, B, C, D, z, dt_bias, softplus, state, load_state, T, n, b, e, workspace, out)
-    _check(load_library().selective_scan_fwd(a, _stream(stream)))
-    return y
+    dev, dtype, code = _first(u)
+    T, n, b, e = _sequences(u, dev, offsets, begin, end)
+    return _scan("selective_scan_fwd", u, dt, A, B, C, D, z, dt_bias, softplus, state, load_state, dev, dtype, code, T,
+                 n, b, e, workspace, out, stream)
 
 
 def selective_scan_step(u, dt, A, B, C, state, D=None, z=None, dt_bias=None, softplus=False, out=None, stream=None):
     """One token of each of N sequences (selective_scan_step): u, dt, z (N, D),
     B, C (N, G, S) or (N, S), state (N, D, S) read and updated in place."""
-    _on_current(u)
+    dev, dtype, code = _first(u)
+    if u.dim() != 2:
+        raise ValueError("u is (N, D)")
     n = u.shape[0]
-    y, a = _scan_args(u, dt, A, B, C, D, z, dt_bias, softplus, state, True, n, n, 0, 0, None, out)
-    _check(load_library().selective_scan_step(a, _stream(stream)))
-    return y
+    return _scan("selective_scan_step", u, dt, A, B, C, D, z, dt_bias, softplus, state, True, dev, dtype, code, n, n, 0,
+                 0, None, out, stream)
 
 
 def matvec_w4(x, q, scale, zero=None, out=None, stream=None):
@@ -733,21 +756,17 @@ def matvec_w4(x, q, scale, zero=None, out=None, stream=None):
     (C,), q (K, C / 2) uint8 with the even channel in the low four bits, scale
     (K, C / group) of x's type, zero the same shape in uint8 (None: 8).
     Returns (M, K) or (K,)."""
-    import torch
-    _on_current(x)
-    if x.dim() not in (1, 2):
+    dev, dtype, code = _first(x)
+    shape, K, groups, u8 = x.shape, q.shape[0], scale.shape[-1], _torch.uint8
+    if len(shape) not in (1, 2):
         raise ValueError("x is (M, C) or (C,)")
-    C, K = x.shape[-1], q.shape[0]
-    M = 1 if x.dim() == 1 else x.shape[0]
-    groups = scale.shape[-1]
+    C, M = shape[-1], shape[0] if len(shape) == 2 else 1
     if groups < 1 or C % groups:
         raise ValueError(f"{groups} groups do not divide {C} channels")
-    y = _like_rows(out, (K,) if x.dim() == 1 else (M, K), "out", x)
-    xp, ldx = _rows_of(x, "x")
-    yp, ldy = _rows_of(y, "out", x)
-    dev = x.device
-    a = _W4.pack(xp, _dense_of(q, "q", (K, C // 2), torch.uint8, dev), _dense_of(scale, "scale", (K, groups), x.dtype, dev),
-                 _dense_of(zero, "zero", (K, groups), torch.uint8, dev), yp, ldx, ldy, M, C, K, C // groups,
-                 _dtype_code(x), 0)
-    _check(load_library().matvec_w4_fwd(a, _stream(stream)))
-    return y
+    xp, ldx = _rows_of(x, "x", shape, dtype, dev)
+    out, yp, ldy = _out_rows(out, (M, K) if len(shape) == 2 else (K,), x, dtype, dev)
+    _seq_call("matvec_w4_fwd", _W4.pack(xp, _dense_of(q, "q", (K, C // 2), u8, dev),
+                                        _dense_of(scale, "scale", (K, groups), dtype, dev),
+                                        _dense_of(zero, "zero", (K, groups), u8, dev), yp, ldx, ldy, M, C, K,
+                                        C // groups, code, 0), dev, stream)
+    return out
