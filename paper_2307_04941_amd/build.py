@@ -25,7 +25,7 @@ SOURCES = ["conv_b3.hip", "conv_b3_fused.hip", "conv_b3_any.hip", "conv_b3_any_f
            "conv_hwcn_vecn_tap_fused.hip", "conv_hwcn_vecn_fused.hip", "conv_hwcn_other_fused.hip",
            "conv_nchw_fused.hip", "conv_nchw_tap.hip", "conv_nchw_tap_fused.hip", "conv_hwcn_persist.hip", "conv_hwcn_persist_fused.hip",
            "conv_launch.hip", "pool.hip", "layout.hip", "plan.cpp", "abi.cpp", "net.cpp", "noalloc.hip", "measure.hip",
-           "conv1d.hip", "scan.hip", "matvec_w4.hip", "seq.cpp"]
+           "conv1d.hip", "scan.hip", "scan_f32.hip", "scan_bf16.hip", "scan_f16.hip", "matvec_w4.hip", "seq.cpp"]
 
 HIPCC = os.environ.get("HIPCC", "/opt/rocm/bin/hipcc")
 ARCH = "gfx950"

@@ -1,69 +1,254 @@
-// Selective state space scan (include/mg3m_seq.h).
-#include "seq_device.h"
+// Selective state space scan (include/mg3m_seq.h): how a prompt is dealt out,
+// the small kernels around scan_pieces (scan_kernel.h), single tokens.
+#include "scan.h"
 
 namespace mg3m {
+namespace {
 
-// One wave per sequence and channel walks the tokens; lane l holds the states
-// l, l + 64, ... and the wave sums their outputs.
-template <typename T>
-__global__ __launch_bounds__(64) void scan_seq(mg3m_scan a) {
-  const int d = blockIdx.x, n = blockIdx.y, lane = threadIdx.x;
-  const int g = d / (a.D / a.G);
-  const SeqRange r = seq_range(a.begin, a.end, n, a.N, a.T);
-  float A[4], h[4];
-  float* state = a.state != nullptr ? a.state + ((long long)n * a.D + d) * a.S : nullptr;
-#pragma unroll
-  for (int i = 0; i < 4; ++i) {
-    const int s = lane + 64 * i;
-    A[i] = s < a.S ? a.A[(long long)d * a.S + s] * kLog2e : 0.0f;
-    h[i] = s < a.S && state != nullptr && a.load_state ? state[s] : 0.0f;
+struct ScanPlan {
+  int P, F;      // states per wave, waves
+  int W;         // tokens per piece, 0: whole sequences
+};
+
+constexpr int pow2_at_least(int v) {
+  int p = 1;
+  while (p < v) p *= 2;
+  return p;
+}
+
+// How many states a wave takes, and whether sequences are cut.
+//
+// Two states per wave and eight waves fill the registers least and share the
+// per-channel work best up to S = 16; more states go to more waves, sixteen at
+// most.  Where there are many work-groups anyway, four states per wave cost
+// less in shared work (64 sequences of 512, D = 4096: 545 us against 613; 4 of
+// 4096, D = 4096: 536 against 397).
+//
+// A work-group walks a whole sequence if that gives nearly every compute unit
+// one (4 of 4096, D = 4096: 397 us whole, 469 cut, though the cut one computes
+// nearly all decays twice).  Else sequences are cut into about two pieces per
+// compute unit: not under 32 tokens, where the kernels' start counts, nor over
+// 256, nor into more than 64 pieces, which are joined one after the other (1
+// of 2048, D = 2048: 63 us in pieces of 128, 72 of 64, 280 whole).
+ScanPlan scan_plan(int T, int D, int G, int S, int N, bool equal) {
+  const double groups = (double)N * G * ((D / G + 63) / 64);
+  // the longest sequence; unknown lengths: four times the average
+  const double longest = equal ? T / N : std::min<double>(T, 4.0 * T / N + 1);
+  ScanPlan s{};
+  s.P = S <= 16 ? (groups >= 2048 ? 4 : 2) : S <= 32 ? 4 : S <= 128 ? 8 : 16;
+  s.F = std::max(2, pow2_at_least((S + s.P - 1) / s.P));
+  if (groups < 224) {
+    s.W = 32;
+    while (s.W < 256 && (s.W < longest * groups / 512 || s.W < longest / 64)) s.W *= 2;
+    if (s.W >= longest) s.W = 0;
   }
-  const float skip = a.D_skip != nullptr ? a.D_skip[d] : 0.0f;
-  const float bias = a.dt_bias != nullptr ? a.dt_bias[d] : 0.0f;
-  for (long long t = r.b; t < r.e; ++t) {
-    const float u = (float)static_cast<const T*>(a.u)[t * a.ldu + d];
-    float delta = (float)static_cast<const T*>(a.dt)[t * a.lddt + d] + bias;
-    if (a.softplus) delta = softplus(delta);
-    float y = 0.0f;
+  return s;
+}
+
+size_t round16(size_t v) { return (v + 255) / 256 * 256; }
+
+struct ScanSpace {
+  size_t bc, slots, sums;      // bytes
+  size_t total() const { return bc + slots + sums; }
+};
+ScanSpace scan_space(const ScanPlan& s, int T, int D, int G, int S, int N, bool equal) {
+  const int some = 0;
+  ScanSpace m{};
+  m.bc = round16(8ull * G * s.F * s.P * T + 128);     // the last tile reads 128 bytes ahead
+  if (s.W != 0) {
+    const size_t ids = (size_t)piece_count(equal ? nullptr : &some, N, T, s.W);
+    m.slots = round16(4ull * ids * D * S);
+    m.sums = round16(4ull * ids * D);
+  }
+  return m;
+}
+
+// bc[g][f][t][2][P] = B, C of the states f * P .. in fp32, zeros behind S: a
+// state behind S stays zero and adds zero.
+template <typename T>
+__global__ __launch_bounds__(256) void scan_pack(ScanArgs a, float* bc, int P, int F) {
+  const long long i = (long long)blockIdx.x * 256 + threadIdx.x;
+  const int w = (int)(i % (2 * P));
+  const long long row = i / (2 * P);
+  const int t = (int)(row % a.p.T);
+  const int gf = (int)(row / a.p.T);
+  if (gf >= a.p.G * F) return;
+  const int g = gf / F, s = (gf - g * F) * P + (w < P ? w : w - P);
+  float v = 0.0f;
+  if (s < a.p.S)
+    v = w < P ? (float)static_cast<const T*>(a.p.B)[t * a.p.ldb + g * a.p.S + s]
+              : (float)static_cast<const T*>(a.p.C)[t * a.p.ldc + g * a.p.S + s];
+  bc[i] = v;
+}
+
+// The states that a sequence's pieces start from: the first one's is the
+// sequence's, the next one's the piece's end state with what is left of its
+// start, exp(A * sum of its step sizes).  slots: end states in, start states
+// out.
+__global__ __launch_bounds__(256) void scan_join(ScanArgs a) {
+  const mg3m_scan& p = a.p;
+  const int i = blockIdx.x * 256 + threadIdx.x, n = blockIdx.y;
+  if (i >= p.D * p.S) return;
+  const int s = i / p.D, d = i - s * p.D;
+  const SeqRange r = seq_range(p.begin, p.end, n, p.N, p.T);
+  const int pieces = max(1, (r.e - r.b + a.W - 1) / a.W);
+  const long long id0 = p.begin == nullptr ? (long long)n * pieces : piece_base(p.begin, n, p.T, a.W);
+  const float A = p.A[(long long)d * p.S + s] * kLog2e;
+  float h = p.load_state ? p.state[((long long)n * p.D + d) * p.S + s] : 0.0f;
+  float* slot = a.slots + (id0 * p.S + s) * p.D + d;
+  const float* sum = a.sums + id0 * p.D + d;
+  const long long step = (long long)p.S * p.D;
+  for (int k = 0; k + 1 < pieces; ++k) {
+    const float end = slot[k * step];
+    slot[k * step] = h;
+    h = fmaf(__builtin_amdgcn_exp2f(A * sum[(long long)k * p.D]), h, end);
+  }
+  slot[(pieces - 1) * step] = h;
+}
+
+ScanFn kernel_of(int dtype, const ScanPlan& s, bool ends) {
+  switch (dtype) {
+    case MG3M_F32: return scan_kernel_f32(s.P, s.F, ends);
+    case MG3M_BF16: return scan_kernel_bf16(s.P, s.F, ends);
+    default: return scan_kernel_f16(s.P, s.F, ends);
+  }
+}
+
+// Single tokens: a lane holds four states of a channel, so a channel takes
+// the next power of two of S / 4 lanes, which then sum its output.  Bound by
+// the states' bytes.
+template <typename T, bool VEC>
+__global__ __launch_bounds__(256) void scan_token(mg3m_scan p, int lanes_log2) {
+  const long long i = (long long)blockIdx.x * 256 + threadIdx.x;
+  const int lanes = 1 << lanes_log2, q = (int)(i & (lanes - 1));
+  long long row = i >> lanes_log2;                  // sequence and channel
+  const bool live = row < (long long)p.N * p.D;
+  if (!live) row = 0;
+  const int n = (int)(row / p.D), d = (int)(row - (long long)n * p.D), s0 = 4 * q;
+  const int g = d / (p.D / p.G);
+  float* state = p.state + row * p.S + s0;
+  const float* rate = p.A + (long long)d * p.S + s0;
+  const T* B = static_cast<const T*>(p.B) + n * p.ldb + g * p.S + s0;
+  const T* C = static_cast<const T*>(p.C) + n * p.ldc + g * p.S + s0;
+  float4 h{}, A{};
+  float b[4] = {}, c[4] = {};
+  if constexpr (VEC) {
+    if (s0 < p.S) {
+      h = *reinterpret_cast<const float4*>(state);
+      A = *reinterpret_cast<const float4*>(rate);
 #pragma unroll
-    for (int i = 0; i < 4; ++i) {
-      const int s = lane + 64 * i;
-      if (s < a.S) {
-        const float B = (float)static_cast<const T*>(a.B)[t * a.ldb + g * a.S + s];
-        const float C = (float)static_cast<const T*>(a.C)[t * a.ldc + g * a.S + s];
-        h[i] = fmaf(__builtin_amdgcn_exp2f(delta * A[i]), h[i], delta * u * B);
-        y = fmaf(C, h[i], y);
+      for (int k = 0; k < 4; ++k) {
+        b[k] = (float)B[k];
+        c[k] = (float)C[k];
       }
     }
-    for (int o = 32; o > 0; o >>= 1) y += __shfl_xor(y, o);
-    y = fmaf(skip, u, y);
-    if (a.z != nullptr) {
-      const float z = (float)static_cast<const T*>(a.z)[t * a.ldz + d];
-      y *= z * sigmoid(z);
-    }
-    if (lane == 0) static_cast<T*>(a.y)[t * a.ldy + d] = (T)y;
-  }
-  if (state != nullptr) {
+  } else {
 #pragma unroll
-    for (int i = 0; i < 4; ++i)
-      if (lane + 64 * i < a.S) state[lane + 64 * i] = h[i];
+    for (int k = 0; k < 4; ++k)
+      if (s0 + k < p.S) {
+        (&h.x)[k] = state[k];
+        (&A.x)[k] = rate[k];
+        b[k] = (float)B[k];
+        c[k] = (float)C[k];
+      }
+  }
+  const float u = (float)static_cast<const T*>(p.u)[n * p.ldu + d];
+  float delta = (float)static_cast<const T*>(p.dt)[n * p.lddt + d];
+  if (p.dt_bias != nullptr) delta += p.dt_bias[d];
+  if (p.softplus) delta = softplus(delta);
+  const float du = delta * u;
+  float out = 0.0f;
+#pragma unroll
+  for (int k = 0; k < 4; ++k) {
+    const float next = fmaf(__builtin_amdgcn_exp2f(delta * ((&A.x)[k] * kLog2e)), (&h.x)[k], du * b[k]);
+    (&h.x)[k] = next;
+    if (s0 + k < p.S) out = fmaf(c[k], next, out);
+  }
+  for (int o = 1; o < lanes; o *= 2) out += __shfl_xor(out, o);
+  if (!live) return;
+  if constexpr (VEC) {
+    if (s0 < p.S) *reinterpret_cast<float4*>(state) = h;
+  } else {
+#pragma unroll
+    for (int k = 0; k < 4; ++k)
+      if (s0 + k < p.S) state[k] = (&h.x)[k];
+  }
+  if (q == 0) {
+    if (p.D_skip != nullptr) out = fmaf(p.D_skip[d], u, out);
+    if (p.z != nullptr) {
+      const float z = (float)static_cast<const T*>(p.z)[n * p.ldz + d];
+      out *= z * sigmoid(z);
+    }
+    static_cast<T*>(p.y)[n * p.ldy + d] = (T)out;
   }
 }
 
-size_t scan_workspace_bytes(int, int, int, int, int) { return 0; }
+bool aligned16(const void* p) { return reinterpret_cast<uintptr_t>(p) % 16 == 0; }
 
-int launch_scan(const mg3m_scan& a, void*, void* stream, std::string* err) {
-  return with_dtype(a.dtype, [&](auto t) {
-    scan_seq<decltype(t)><<<dim3(a.D, a.N), 64, 0, static_cast<hipStream_t>(stream)>>>(a);
+}  // namespace
+
+size_t scan_workspace_bytes(int T, int D, int G, int S, int N) {
+  // for equal parts and for given rows, whichever takes more
+  size_t most = 0;
+  for (bool equal : {true, false})
+    most = std::max(most, scan_space(scan_plan(T, D, G, S, N, equal), T, D, G, S, N, equal).total());
+  return most;
+}
+
+int launch_scan(const mg3m_scan& p, void* ws, void* stream, std::string* err) {
+  hipStream_t st = static_cast<hipStream_t>(stream);
+  const bool equal = p.begin == nullptr;
+  const ScanPlan s = scan_plan(p.T, p.D, p.G, p.S, p.N, equal);
+  const ScanSpace m = scan_space(s, p.T, p.D, p.G, p.S, p.N, equal);
+  ScanArgs a{};
+  a.p = p;
+  char* at = static_cast<char*>(ws);
+  float* bc = reinterpret_cast<float*>(at);
+  a.bc = bc;
+  a.slots = reinterpret_cast<float*>(at + m.bc);
+  a.sums = reinterpret_cast<float*>(at + m.bc + m.slots);
+  a.W = s.W;
+  a.blocks = (p.D / p.G + 63) / 64;
+  const long long groups = piece_count(p.begin, p.N, p.T, s.W) * p.G * a.blocks;
+  const long long pack = ((long long)p.G * s.F * p.T * 2 * s.P + 255) / 256;
+  if (groups > 0x7fffffffLL || pack > 0x7fffffffLL || p.N > 65535) {
+    *err = "selective scan: too many rows, sequences or channels for one launch";
+    return MG3M_ERR_TOO_LARGE;
+  }
+  const ScanFn ends = kernel_of(p.dtype, s, true), whole = kernel_of(p.dtype, s, false);
+  if (ends == nullptr || whole == nullptr) {
+    *err = "selective scan: no kernel for this plan";
+    return MG3M_ERR_PLAN;
+  }
+  if (pack > 0) {
+    with_dtype(p.dtype, [&](auto t) {
+      scan_pack<decltype(t)><<<(unsigned)pack, 256, 0, st>>>(a, bc, s.P, s.F);
+      return 0;
+    });
+  }
+  if (s.W != 0) {
+    ends<<<(unsigned)groups, 64 * s.F, 0, st>>>(a);
+    scan_join<<<dim3((p.D * p.S + 255) / 256, p.N), 256, 0, st>>>(a);
+  }
+  whole<<<(unsigned)groups, 64 * s.F, 0, st>>>(a);
+  return launched("selective scan", err);
+}
+
+int launch_scan_step(const mg3m_scan& p, void* stream, std::string* err) {
+  int lanes_log2 = 0;
+  while (4 << lanes_log2 < p.S) ++lanes_log2;
+  const long long groups = (((long long)p.N * p.D << lanes_log2) + 255) / 256;
+  if (groups > 0x7fffffffLL) {
+    *err = "selective scan: too many sequences and channels for one launch";
+    return MG3M_ERR_TOO_LARGE;
+  }
+  const bool vec = p.S % 4 == 0 && aligned16(p.state) && aligned16(p.A);
+  return with_dtype(p.dtype, [&](auto t) {
+    using T = decltype(t);
+    auto* kernel = vec ? scan_token<T, true> : scan_token<T, false>;
+    kernel<<<(unsigned)groups, 256, 0, static_cast<hipStream_t>(stream)>>>(p, lanes_log2);
     return launched("selective scan", err);
   });
-}
-
-int launch_scan_step(const mg3m_scan& a, void* stream, std::string* err) {
-  mg3m_scan s = a;
-  s.T = a.N;
-  s.load_state = 1;
-  return launch_scan(s, nullptr, stream, err);
 }
 
 }  // namespace mg3m
