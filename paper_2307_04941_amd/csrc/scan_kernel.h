@@ -155,7 +155,7 @@ __global__ __launch_bounds__(64 * F) void scan_pieces(ScanArgs a) {
   auto part_tile = [&](int tile, int some, auto&& get, auto&& put) {
 #pragma unroll 1
     for (int j = 0; j < some; ++j) {
-      const float* at = bc + (long long)(tile * kTile + j) * 2 * P;
+      const auto* at = (const __attribute__((address_space(4))) float*)(bc + (long long)(tile * kTile + j) * 2 * P);
       const float2 x = get(j);
       float decay[P];
       decays(x.x, decay);
