@@ -16,8 +16,11 @@
 // A work-group has eight waves: RW tiles of 16 weight rows times CW slices of
 // the channels, whose sums are joined through LDS in a fixed order.  It keeps
 // x in LDS in the order the matrix instruction takes it, eight channels of a
-// token together, permuted as the weights come out of a dword; long rows in
-// slabs.  A wave has four blocks of 128 channels of weights under way.
+// token together, permuted as the weights come out of a dword, and the rows'
+// scales, as s and s (16 + zero); long rows in slabs.  A wave has four blocks
+// of 128 channels of weights under way.
+#include <type_traits>
+
 #include "seq_device.h"
 
 namespace mg3m {
@@ -35,7 +38,12 @@ struct W4Args {
   mg3m_w4 p;
   int slab_log2;   // units of x in LDS, CW at least
   int vec;         // x rows are 16-byte aligned
+  unsigned per_group;      // ceil(2^31 / (group / 32))
+
+  // The group of a block of 32 channels: exact for block * (group / 32) below 2^31.
+  __device__ __forceinline__ int group_of(int block) const { return (int)__umulhi(2u * block, per_group); }
 };
+constexpr int kMaxChannels = 1 << 20;
 
 template <typename T>
 struct W4Type;
@@ -107,116 +115,151 @@ __device__ __forceinline__ void arrange(const T (&v)[8], u32x4 (&out)[W4Type<T>:
 
 // WHOLE: a group covers whole units.  Otherwise the lanes' dwords are
 // transposed (lane quarter against dword), after which an MFMA covers 32
-// consecutive channels, which lie in one group.
-template <typename T, int RW, int CW, bool WHOLE>
+// consecutive channels, which lie in one group.  MT: tokens that LDS has room
+// for, so that its addresses differ by constants.
+template <typename T, int MT, int RW, int CW, bool WHOLE>
 __global__ __launch_bounds__(512) void matvec_w4(W4Args a) {
-  constexpr int kParts = W4Type<T>::kParts;
-  extern __shared__ u32x4 xs[];                  // [unit][part][16 blocks of 8 channels][tokens]
+  constexpr int kParts = W4Type<T>::kParts, kRows = 16 * RW;
+  extern __shared__ u32x4 xs[];                  // [unit][part][16 blocks of 8 channels][MT], then ss
   const mg3m_w4& p = a.p;
   const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
   const int rw = wave / CW, cw = wave - rw * CW;
   const int col = lane & 15, quarter = lane >> 4;
-  const int row_blocks = (p.K + 16 * RW - 1) / (16 * RW);
-  const int mb = blockIdx.x / row_blocks;
+  const int row_blocks = (p.K + kRows - 1) / kRows;
+  const int mb = blockIdx.x / row_blocks, row0 = (int)(blockIdx.x - mb * row_blocks) * kRows;
   const int m0 = mb * 16, tokens = min(16, p.M - m0);
-  const int row = (int)(blockIdx.x - mb * row_blocks) * (16 * RW) + rw * 16 + col;
-  const bool live = row < p.K;
-  const long long r = min(row, p.K - 1);
+  const int row = row0 + rw * 16 + col;
   const int units = (p.C + kUnit - 1) / kUnit, groups = p.C / p.group;
-  const unsigned char* q = p.q + r * (p.C / 2);
-  const T* scale = static_cast<const T*>(p.scale) + r * groups;
-  const unsigned char* zero = p.zero != nullptr ? p.zero + r * groups : nullptr;
+  const unsigned char* q = p.q + (long long)min(row, p.K - 1) * (p.C / 2);
   const int token = min(col, tokens - 1);        // columns behind the last token repeat it
+  const int slab = 1 << a.slab_log2, per_slab = slab / CW;      // per_slab: a multiple of kAhead
+  float2* ss = reinterpret_cast<float2*>(xs + (kParts * 16 * MT << a.slab_log2));     // [group][row]
 
-  // unit i of this wave; behind the end the row's first bytes, against x = 0
-  auto weights = [&](int i) {
-    const int c = (i * CW + cw) * kUnit + quarter * 32;
-    return *reinterpret_cast<const u32x4*>(q + (c < p.C ? c / 2 : 0));
-  };
-  u32x4 w[kAhead];
+  // Four units of this wave from unit i of a slab; behind the end the row's
+  // first bytes, against x = 0.
+  auto load = [&](int unit0, int i, u32x4 (&w)[kAhead]) {
 #pragma unroll
-  for (int i = 0; i < kAhead; ++i) w[i] = weights(i);
-
-  const u32x4 ones = {W4Type<T>::kOnes, W4Type<T>::kOnes, W4Type<T>::kOnes, W4Type<T>::kOnes};
-  f32x4 y = {};
-  const int slab = 1 << a.slab_log2, per_slab = slab / CW;
-  const int rounds = ((units + slab - 1) >> a.slab_log2) * per_slab;     // the same for all waves
-
-  auto stage = [&](int unit0) {
-    const int blocks = min(slab, units - unit0) * (kUnit / 8), row_log2 = a.slab_log2 + 4;
-    for (int i = threadIdx.x; i < tokens << row_log2; i += 512) {
-      const int m = i >> row_log2, b = i & ((1 << row_log2) - 1);
-      if (b >= blocks) continue;
-      const int c = unit0 * kUnit + b * 8;
-      const T* x = static_cast<const T*>(p.x) + (m0 + m) * p.ldx + c;
-      T v[8];
-      if (c < p.C) {
-        if (a.vec) {
-#pragma unroll
-          for (int k = 0; k < (int)sizeof(T) / 2; ++k)
-            *reinterpret_cast<u32x4*>(v + k * 16 / sizeof(T)) = reinterpret_cast<const u32x4*>(x)[k];
-        } else {
-#pragma unroll
-          for (int k = 0; k < 8; ++k) v[k] = x[k];
-        }
-      } else {
-#pragma unroll
-        for (int k = 0; k < 8; ++k) v[k] = (T)0.0f;
-      }
-      u32x4 o[kParts];
-      arrange(v, o);
-      const int u = b / 16;
-#pragma unroll
-      for (int part = 0; part < kParts; ++part) xs[((u * kParts + part) * 16 + b % 16) * tokens + m] = o[part];
+    for (int k = 0; k < kAhead; ++k) {
+      const int c = (unit0 + (i + k) * CW + cw) * kUnit + quarter * 32;
+      w[k] = *reinterpret_cast<const u32x4*>(q + (c < p.C ? c / 2 : 0));
     }
   };
 
-  for (int i0 = 0; i0 < rounds; i0 += kAhead) {
+  // Four loads at a time; those behind the end repeat an element.
+  auto stage_scales = [&](int group0, int here) {
+    constexpr int kPer = 512 / kRows;            // threads on a row's scales
+    const int k = threadIdx.x / kPer;
+    const long long at = (long long)min(row0 + k, p.K - 1) * groups + group0;
+    const unsigned char* zero = p.zero != nullptr ? p.zero : p.q;     // q: read, not used
+    for (int g0 = threadIdx.x % kPer; g0 < here; g0 += 4 * kPer) {
+      float s[4], z[4];
 #pragma unroll
-    for (int k = 0; k < kAhead; ++k) {
-      const int i = i0 + k;
-      if (i >= rounds) break;
-      if ((i & (per_slab - 1)) == 0) {
-        if (i > 0) __syncthreads();
-        stage(i * CW);
-        __syncthreads();
+      for (int n = 0; n < 4; ++n) {
+        const int g = min(g0 + n * kPer, here - 1);
+        s[n] = (float)static_cast<const T*>(p.scale)[at + g];
+        z[n] = (float)zero[at + g];
       }
-      const int unit = i * CW + cw;
-      if (unit < units) {
-        u32x4 v = w[k];
-        if constexpr (!WHOLE) {
-          const auto s02 = __builtin_amdgcn_permlane32_swap(v[0], v[2], false, false);
-          const auto s13 = __builtin_amdgcn_permlane32_swap(v[1], v[3], false, false);
-          const auto s01 = __builtin_amdgcn_permlane16_swap(s02[0], s13[0], false, false);
-          const auto s23 = __builtin_amdgcn_permlane16_swap(s02[1], s13[1], false, false);
-          v = u32x4{s01[0], s01[1], s23[0], s23[1]};
-        }
-        const u32x4* x = xs + (unit & (slab - 1)) * kParts * 16 * tokens + token;
-        auto scaled = [&](f32x4 dot, f32x4 sum, int c) {
-          const int g = min(c, p.C - 1) / p.group;
-          const float s = (float)scale[g], z = 16.0f + (zero != nullptr ? (float)zero[g] : 8.0f);
 #pragma unroll
-          for (int e = 0; e < 4; ++e) y[e] = fmaf(s, fmaf(-z, sum[e], dot[e]), y[e]);
-        };
-        f32x4 dot = {}, sum = {};
-#pragma unroll
-        for (int d = 0; d < 4; ++d) {
-          const u32x4 b = expand<T>(v[d]);
-          const int block = WHOLE ? quarter * 4 + d : d * 4 + quarter;
-#pragma unroll
-          for (int part = 0; part < kParts; ++part) {
-            const u32x4 xa = x[(part * 16 + block) * tokens];
-            dot = mfma<T>(xa, b, dot);
-            sum = mfma<T>(xa, ones, sum);
-          }
-          if constexpr (!WHOLE) {
-            scaled(dot, sum, unit * kUnit + d * 32);
-            dot = sum = f32x4{};
-          }
-        }
-        if constexpr (WHOLE) scaled(dot, sum, unit * kUnit);
+      for (int n = 0; n < 4; ++n) {
+        const float z16 = 16.0f + (p.zero != nullptr ? z[n] : 8.0f);
+        if (g0 + n * kPer < here) ss[(g0 + n * kPer) * kRows + k] = float2{s[n], s[n] * z16};
       }
-      w[k] = weights(i + kAhead);
+    }
+  };
+  // Channels behind the last one are zeros, to the slab's end.
+  auto stage_x = [&](int unit0, auto vec) {
+    const int row_log2 = a.slab_log2 + 4;
+    for (int i0 = threadIdx.x; i0 < tokens << row_log2; i0 += 4 * 512) {
+      T v[4][8];
+#pragma unroll
+      for (int n = 0; n < 4; ++n) {
+        const int i = i0 + n * 512, b = i & ((1 << row_log2) - 1);
+        const int m = min(i >> row_log2, tokens - 1), c = min(unit0 * kUnit + b * 8, p.C - 8);
+        const T* x = static_cast<const T*>(p.x) + (m0 + m) * p.ldx + c;
+        if constexpr (decltype(vec)::value) {
+#pragma unroll
+          for (int k = 0; k < (int)sizeof(T) / 2; ++k)
+            *reinterpret_cast<u32x4*>(v[n] + k * 16 / sizeof(T)) = reinterpret_cast<const u32x4*>(x)[k];
+        } else {
+#pragma unroll
+          for (int k = 0; k < 8; ++k) v[n][k] = x[k];
+        }
+      }
+#pragma unroll
+      for (int n = 0; n < 4; ++n) {
+        const int i = i0 + n * 512, m = i >> row_log2, b = i & ((1 << row_log2) - 1);
+        if (m >= tokens) continue;
+        u32x4 o[kParts];
+        arrange(v[n], o);
+        const bool in = unit0 * kUnit + b * 8 < p.C;
+#pragma unroll
+        for (int part = 0; part < kParts; ++part)
+          xs[((b / 16 * kParts + part) * 16 + b % 16) * MT + m] = in ? o[part] : u32x4{};
+      }
+    }
+  };
+
+  const u32x4 ones = {W4Type<T>::kOnes, W4Type<T>::kOnes, W4Type<T>::kOnes, W4Type<T>::kOnes};
+  f32x4 y = {};
+  int group0 = 0;                                // the slab's first group
+  auto product = [&](int unit0, int in_slab, u32x4 v) {
+    const u32x4* x = xs + in_slab * (kParts * 16 * MT) + quarter * (WHOLE ? 4 * MT : MT) + token;
+    u32x4 xa[4][kParts];
+    float2 s[WHOLE ? 1 : 4];
+#pragma unroll
+    for (int d = 0; d < 4; ++d) {
+#pragma unroll
+      for (int part = 0; part < kParts; ++part) xa[d][part] = x[(part * 16 + (WHOLE ? d : 4 * d)) * MT];
+    }
+#pragma unroll
+    for (int d = 0; d < (WHOLE ? 1 : 4); ++d) {
+      const int g = a.group_of(min((unit0 + in_slab) * 4 + d, p.C / 32 - 1)) - group0;
+      s[d] = ss[g * kRows + rw * 16 + col];
+    }
+    if constexpr (!WHOLE) {
+      const auto s02 = __builtin_amdgcn_permlane32_swap(v[0], v[2], false, false);
+      const auto s13 = __builtin_amdgcn_permlane32_swap(v[1], v[3], false, false);
+      const auto s01 = __builtin_amdgcn_permlane16_swap(s02[0], s13[0], false, false);
+      const auto s23 = __builtin_amdgcn_permlane16_swap(s02[1], s13[1], false, false);
+      v = u32x4{s01[0], s01[1], s23[0], s23[1]};
+    }
+    f32x4 dot = {}, sum = {};
+#pragma unroll
+    for (int d = 0; d < 4; ++d) {
+      const u32x4 b = expand<T>(v[d]);
+#pragma unroll
+      for (int part = 0; part < kParts; ++part) {
+        dot = mfma<T>(xa[d][part], b, dot);
+        sum = mfma<T>(xa[d][part], ones, sum);
+      }
+      if (!WHOLE || d == 3) {
+        const float2 f = s[WHOLE ? 0 : d];
+#pragma unroll
+        for (int e = 0; e < 4; ++e) y[e] = fmaf(f.x, dot[e], fmaf(-f.y, sum[e], y[e]));
+        dot = sum = f32x4{};
+      }
+    }
+  };
+  for (int unit0 = 0; unit0 < units; unit0 += slab) {
+    u32x4 w0[kAhead], w1[kAhead];
+    load(unit0, 0, w0);
+    group0 = a.group_of(unit0 * (kUnit / 32));
+    const int end = min((min(unit0 + slab, units)) * kUnit, p.C);
+    if (unit0 > 0) __syncthreads();
+    stage_scales(group0, a.group_of(end / 32 - 1) - group0 + 1);
+    if (a.vec) stage_x(unit0, std::true_type{});
+    else stage_x(unit0, std::false_type{});
+    __syncthreads();
+    // this wave's units of the slab, with those of zeros that fill the last four
+    const int mine = min(per_slab, (units - unit0 + CW - 1) / CW);
+    for (int i = 0; i < mine; i += 2 * kAhead) {
+      if (i + kAhead < mine) load(unit0, i + kAhead, w1);
+#pragma unroll
+      for (int k = 0; k < kAhead; ++k) product(unit0, (i + k) * CW + cw, w0[k]);
+      if (i + kAhead >= mine) break;
+      if (i + 2 * kAhead < mine) load(unit0, i + 2 * kAhead, w0);
+#pragma unroll
+      for (int k = 0; k < kAhead; ++k) product(unit0, (i + kAhead + k) * CW + cw, w1[k]);
     }
   }
 
@@ -230,7 +273,7 @@ __global__ __launch_bounds__(512) void matvec_w4(W4Args a) {
 #pragma unroll
     for (int c = 1; c < CW; ++c) y += join[(rw * CW + c) * 64 + lane];
   }
-  if (!live) return;
+  if (row >= p.K) return;
 #pragma unroll
   for (int e = 0; e < 4; ++e) {
     const int m = quarter * 4 + e;
@@ -238,7 +281,7 @@ __global__ __launch_bounds__(512) void matvec_w4(W4Args a) {
   }
 }
 
-template <typename T, int RW, int CW>
+template <typename T, int MT, int RW, int CW>
 int launch_w4_as(W4Args a, void* stream, std::string* err) {
   const mg3m_w4& p = a.p;
   const long long groups = (long long)((p.K + 16 * RW - 1) / (16 * RW)) * ((p.M + 15) / 16);
@@ -246,30 +289,44 @@ int launch_w4_as(W4Args a, void* stream, std::string* err) {
     *err = "4-bit product: too many rows for one launch";
     return MG3M_ERR_TOO_LARGE;
   }
-  // x in LDS: all of it, or slabs that leave room for a second work-group
-  const int unit_bytes = std::min(p.M, 16) * kUnit * 2 * W4Type<T>::kParts;
+  // x and scales in LDS: all of them, or slabs that leave room for a second work-group
+  const int x_unit = MT * kUnit * 2 * W4Type<T>::kParts;
   const int units = (p.C + kUnit - 1) / kUnit;
-  static_assert((CW & (CW - 1)) == 0, "slabs are a power of two");
-  while (1 << a.slab_log2 < CW) ++a.slab_log2;
-  while (1 << a.slab_log2 < units && (2 * unit_bytes) << a.slab_log2 <= 65536) ++a.slab_log2;
-  const size_t lds = std::max<size_t>((size_t)unit_bytes << a.slab_log2, CW > 1 ? 8 * 64 * sizeof(f32x4) : 0);
-  const bool whole = p.group % kUnit == 0;
-  auto* kernel = whole ? matvec_w4<T, RW, CW, true> : matvec_w4<T, RW, CW, false>;
+  const auto bytes = [&](int log2) {
+    return ((size_t)x_unit << log2) + (((size_t)kUnit << log2) / p.group + 2) * 16 * RW * sizeof(float2);
+  };
+  while (1 << a.slab_log2 < CW * kAhead) ++a.slab_log2;
+  while (1 << a.slab_log2 < units && bytes(a.slab_log2 + 1) <= 65536) ++a.slab_log2;
+  const size_t lds = std::max<size_t>(bytes(a.slab_log2), CW > 1 ? 8 * 64 * sizeof(f32x4) : 0);
+  auto* kernel = p.group % kUnit == 0 ? matvec_w4<T, MT, RW, CW, true> : matvec_w4<T, MT, RW, CW, false>;
   kernel<<<(unsigned)groups, 512, lds, static_cast<hipStream_t>(stream)>>>(a);
   return launched("4-bit product", err);
+}
+
+template <typename T, int MT>
+int launch_w4_mt(const W4Args& a, long long tiles, void* stream, std::string* err) {
+  if (tiles >= 1024 || MT * W4Type<T>::kParts > 16) return launch_w4_as<T, MT, 4, 2>(a, stream, err);
+  return launch_w4_as<T, MT, 1, 8>(a, stream, err);
 }
 
 }  // namespace
 
 int launch_w4(const mg3m_w4& p, void* stream, std::string* err) {
+  if (p.C > kMaxChannels) {
+    *err = "4-bit product: more than 2^20 channels";
+    return MG3M_ERR_TOO_LARGE;
+  }
   return with_dtype(p.dtype, [&](auto t) {
     using T = decltype(t);
     W4Args a{};
     a.p = p;
     a.vec = reinterpret_cast<uintptr_t>(p.x) % 16 == 0 && (p.ldx * sizeof(T)) % 16 == 0;
+    const unsigned blocks = p.group / 32;
+    a.per_group = ((1u << 31) + blocks - 1) / blocks;
     // wide products share x between four tiles of rows
     const long long tiles = (long long)((p.K + 15) / 16) * ((p.M + 15) / 16);
-    return tiles >= 1024 ? launch_w4_as<T, 4, 2>(a, stream, err) : launch_w4_as<T, 1, 8>(a, stream, err);
+    return p.M == 1 ? launch_w4_mt<T, 1>(a, tiles, stream, err)
+           : p.M <= 4 ? launch_w4_mt<T, 4>(a, tiles, stream, err) : launch_w4_mt<T, 16>(a, tiles, stream, err);
   });
 }
 
