@@ -1,59 +1,172 @@
 // Causal depthwise convolution along tokens (include/mg3m_seq.h).
+//
+// 2 R flops per element: bound by the bytes of x and y.  A thread takes V
+// neighbouring channels (16 bytes, or one where rows are not 16-byte aligned)
+// through a piece of a sequence, the last R inputs of each in registers, so
+// that x is read once but for the R - 1 rows before a piece.
 #include "seq_device.h"
 
 namespace mg3m {
+namespace {
 
-// One thread per sequence and channel walks the tokens with its last R inputs
-// in registers.
-template <typename T, int R>
-__global__ __launch_bounds__(64) void conv1d_seq(mg3m_conv1d a) {
-  const int c = blockIdx.x * 64 + threadIdx.x, n = blockIdx.y;
-  if (c >= a.C) return;
-  const SeqRange r = seq_range(a.begin, a.end, n, a.N, a.T);
-  const T* x = static_cast<const T*>(a.x) + c;
-  T* y = static_cast<T*>(a.y) + c;
-  T* state = a.state != nullptr && R > 1 ? static_cast<T*>(a.state) + (long long)n * (R - 1) * a.C + c : nullptr;
-  float w[R], v[R];
+constexpr int kStep = 4;             // tokens whose loads are issued together
+
+struct ConvArgs {
+  mg3m_conv1d p;
+  int W;               // tokens of a piece, a multiple of kStep
+  int vecs;            // groups of V channels
+  unsigned items;      // pieces times vecs
+};
+
+template <typename T, int V>
+struct alignas(V * sizeof(T)) Pack {
+  T v[V];
+};
+
+template <typename T, int V, int R>
+__global__ __launch_bounds__(256) void conv1d_pieces(ConvArgs a) {
+  const mg3m_conv1d& p = a.p;
+  const unsigned item = blockIdx.x * 256u + threadIdx.x;
+  if (item >= a.items) return;
+  const int id = item / a.vecs, c = (int)(item - id * (unsigned)a.vecs) * V;
+  const Piece pc = find_piece(p.begin, p.end, p.N, p.T, a.W, id);
+  if (pc.n < 0) return;
+
+  using P = Pack<T, V>;
+  const T* x = static_cast<const T*>(p.x) + c;
+  T* y = static_cast<T*>(p.y) + c;
+  T* state = R > 1 && p.state != nullptr ? static_cast<T*>(p.state) + (long long)pc.n * (R - 1) * p.C + c : nullptr;
+  auto row = [&](int t) { return *reinterpret_cast<const P*>(x + (unsigned long long)(unsigned)t * (unsigned)p.ldx); };
+  const int first = pc.b - pc.k * a.W;           // the sequence's first row
+
+  float w[R][V], h[R][V], bias[V];               // h[i]: the input i + 1 - R rows before
 #pragma unroll
-  for (int i = 0; i < R; ++i) w[i] = (float)static_cast<const T*>(a.w)[(long long)i * a.C + c];
+  for (int i = 0; i < R; ++i) {
+    const P r = *reinterpret_cast<const P*>(static_cast<const T*>(p.w) + (long long)i * p.C + c);
 #pragma unroll
-  for (int i = 1; i < R; ++i) v[i] = state != nullptr && a.load_state ? (float)state[(long long)(i - 1) * a.C] : 0.0f;
-  const float bias = a.bias != nullptr ? (float)static_cast<const T*>(a.bias)[c] : 0.0f;
-  for (int t = r.b; t < r.e; ++t) {
-#pragma unroll
-    for (int i = 0; i + 1 < R; ++i) v[i] = v[i + 1];
-    v[R - 1] = (float)x[t * a.ldx];
-    float s = bias;
-#pragma unroll
-    for (int i = 0; i < R; ++i) s = fmaf(w[i], v[i], s);
-    if (a.silu) s *= sigmoid(s);
-    y[t * a.ldy] = (T)s;
+    for (int k = 0; k < V; ++k) w[i][k] = (float)r.v[k];
   }
-  if (state != nullptr) {
+  {
+    P r{};
+    if (p.bias != nullptr) r = *reinterpret_cast<const P*>(static_cast<const T*>(p.bias) + c);
 #pragma unroll
-    for (int i = 1; i < R; ++i) state[(long long)(i - 1) * a.C] = (T)v[i];
+    for (int k = 0; k < V; ++k) bias[k] = (float)r.v[k];
   }
+  // the R - 1 rows before this piece: x's, or at the sequence's start its state's
+#pragma unroll
+  for (int i = 1; i < R; ++i) {
+    const int t = pc.b - R + i;
+    P r{};
+    if (t >= first) r = row(t);
+    else if (state != nullptr && p.load_state) r = *reinterpret_cast<const P*>(state + (long long)(t - first + R - 1) * p.C);
+#pragma unroll
+    for (int k = 0; k < V; ++k) h[i][k] = (float)r.v[k];
+  }
+  // The thread of the first piece has read the sequence's state, so it writes
+  // the one after: rows end - R + 1 .. of state and x together.
+  if (state != nullptr && pc.k == 0) {
+    const SeqRange s = seq_range(p.begin, p.end, pc.n, p.N, p.T);
+#pragma unroll
+    for (int i = 1; i < R; ++i) {
+      const int t = s.e - R + i;
+      P r{};
+      if (t >= first) {
+        r = row(t);
+      } else {
+        const int from = t - first + R;          // h's row: at least i, as the sequence has no rows below 0
+#pragma unroll
+        for (int j = 1; j < R; ++j)
+          if (j == from)
+#pragma unroll
+            for (int k = 0; k < V; ++k) r.v[k] = (T)h[j][k];
+      }
+      *reinterpret_cast<P*>(state + (long long)(i - 1) * p.C) = r;
+    }
+  }
+
+  auto output = [&](int t, const P& in) {
+#pragma unroll
+    for (int i = 0; i + 1 < R; ++i)
+#pragma unroll
+      for (int k = 0; k < V; ++k) h[i][k] = h[i + 1][k];
+    P out;
+#pragma unroll
+    for (int k = 0; k < V; ++k) {
+      h[R - 1][k] = (float)in.v[k];
+      float s = bias[k];
+#pragma unroll
+      for (int i = 0; i < R; ++i) s = fmaf(w[i][k], h[i][k], s);
+      const float act = s * sigmoid(s);
+      out.v[k] = (T)(p.silu ? act : s);
+    }
+    *reinterpret_cast<P*>(y + (unsigned long long)(unsigned)t * (unsigned)p.ldy) = out;
+  };
+  // h moves up with each token: its first row is the oldest
+#pragma unroll
+  for (int k = 0; k < V; ++k) h[0][k] = 0.0f;
+  int t = pc.b;
+  for (; t + kStep <= pc.e; t += kStep) {
+    P in[kStep];
+#pragma unroll
+    for (int j = 0; j < kStep; ++j) in[j] = row(t + j);
+#pragma unroll
+    for (int j = 0; j < kStep; ++j) output(t + j, in[j]);
+  }
+  for (; t < pc.e; ++t) output(t, row(t));
 }
 
-template <typename T>
-static int launch_taps(const mg3m_conv1d& a, void* stream, std::string* err) {
-  const dim3 grid((a.C + 63) / 64, a.N);
+template <typename T, int V>
+void launch_taps(const ConvArgs& a, void* stream) {
+  const unsigned grid = (a.items + 255) / 256;
   hipStream_t st = static_cast<hipStream_t>(stream);
-  switch (a.R) {
-    case 1: conv1d_seq<T, 1><<<grid, 64, 0, st>>>(a); break;
-    case 2: conv1d_seq<T, 2><<<grid, 64, 0, st>>>(a); break;
-    case 3: conv1d_seq<T, 3><<<grid, 64, 0, st>>>(a); break;
-    case 4: conv1d_seq<T, 4><<<grid, 64, 0, st>>>(a); break;
-    case 5: conv1d_seq<T, 5><<<grid, 64, 0, st>>>(a); break;
-    case 6: conv1d_seq<T, 6><<<grid, 64, 0, st>>>(a); break;
-    case 7: conv1d_seq<T, 7><<<grid, 64, 0, st>>>(a); break;
-    default: conv1d_seq<T, 8><<<grid, 64, 0, st>>>(a); break;
+  switch (a.p.R) {
+    case 1: conv1d_pieces<T, V, 1><<<grid, 256, 0, st>>>(a); break;
+    case 2: conv1d_pieces<T, V, 2><<<grid, 256, 0, st>>>(a); break;
+    case 3: conv1d_pieces<T, V, 3><<<grid, 256, 0, st>>>(a); break;
+    case 4: conv1d_pieces<T, V, 4><<<grid, 256, 0, st>>>(a); break;
+    case 5: conv1d_pieces<T, V, 5><<<grid, 256, 0, st>>>(a); break;
+    case 6: conv1d_pieces<T, V, 6><<<grid, 256, 0, st>>>(a); break;
+    case 7: conv1d_pieces<T, V, 7><<<grid, 256, 0, st>>>(a); break;
+    default: conv1d_pieces<T, V, 8><<<grid, 256, 0, st>>>(a); break;
   }
-  return launched("causal convolution", err);
 }
 
-int launch_conv1d(const mg3m_conv1d& a, void* stream, std::string* err) {
-  return with_dtype(a.dtype, [&](auto t) { return launch_taps<decltype(t)>(a, stream, err); });
+bool aligned16(const void* p) { return reinterpret_cast<uintptr_t>(p) % 16 == 0; }
+
+}  // namespace
+
+int launch_conv1d(const mg3m_conv1d& p, void* stream, std::string* err) {
+  return with_dtype(p.dtype, [&](auto t) {
+    using T = decltype(t);
+    constexpr int V = 16 / sizeof(T);
+    const bool vec = p.C % V == 0 && p.ldx % V == 0 && p.ldy % V == 0 && aligned16(p.x) && aligned16(p.y) &&
+                     aligned16(p.w) && aligned16(p.bias) && aligned16(p.state);
+    ConvArgs a{};
+    a.p = p;
+    a.vecs = vec ? p.C / V : p.C;
+    // Pieces as long as they may be with threads enough to fill the chip: each
+    // piece reads R - 1 rows again.  Not under R - 1 tokens: only a sequence's
+    // first piece may read its state, which the same thread overwrites.
+    const int least = p.R - 1 <= kStep ? kStep : 2 * kStep;
+    static_assert(2 * kStep >= 7, "R is at most 8");
+    long long items = 0;
+    for (a.W = 32;; a.W /= 2) {
+      items = piece_count(p.begin, p.N, p.T, a.W) * a.vecs;
+      if (a.W == least || items >= 256 * 2048) break;
+    }
+    while (items > 0x7fffffffLL && a.W < (1 << 20)) {
+      a.W *= 2;
+      items = piece_count(p.begin, p.N, p.T, a.W) * a.vecs;
+    }
+    if (items > 0x7fffffffLL) {
+      *err = "causal convolution: too many sequences and channels for one launch";
+      return (int)MG3M_ERR_TOO_LARGE;
+    }
+    a.items = (unsigned)items;
+    if (vec) launch_taps<T, V>(a, stream);
+    else launch_taps<T, 1>(a, stream);
+    return launched("causal convolution", err);
+  });
 }
 
 int launch_conv1d_step(const mg3m_conv1d& a, void* stream, std::string* err) {
