@@ -2,23 +2,12 @@
 //
 // Bound by the weights' bytes: with one token each weight is used once, with
 // 16 still only 16 times.  What has to be cheap is a weight's way from four
-// bits to a matrix instruction.  v_mfma_f32_16x16x32 takes 16 tokens (rows)
-// times 16 weight rows (columns): a lane holds eight consecutive channels of
-// one row, which is one dword of 4-bit weights, so no weight moves between
-// lanes.  Shifted so that a nibble is the top of a 16-bit float's mantissa
-// under the exponent of 16, w & mask | exponent is the pair of numbers 16 + q,
-// exact in bf16 and in fp16: two instructions for two weights.  The 16 and the
-// zero point leave the sum through a second product, with ones:
+// bits to a product.  Shifted so that a nibble is the top of a 16-bit float's
+// mantissa under the exponent of 16, w & mask | exponent is the pair of numbers
+// 16 + q, exact in bf16 and in fp16: two instructions for two weights.  The 16
+// and the zero point leave the sum through a second one, of the tokens alone,
 //   sum x (q - zero) = sum x (16 + q) - (16 + zero) sum x,
-// whose terms are 31/8 the size of the result's, so two of fp32's 24 bits.
-// fp32 tokens go in as three bf16 parts (exact, as in conv_b3.h).
-//
-// A work-group has eight waves: RW tiles of 16 weight rows times CW slices of
-// the channels, whose sums are joined through LDS in a fixed order.  It keeps
-// x in LDS in the order the matrix instruction takes it, eight channels of a
-// token together, permuted as the weights come out of a dword, and the rows'
-// scales, as s and s (16 + zero); long rows in slabs.  A wave has four blocks
-// of 128 channels of weights under way.
+// whose terms are up to 31/8 the size of the result's: two of fp32's 24 bits.
 #include <type_traits>
 
 #include "seq_device.h"
@@ -32,12 +21,11 @@ typedef __bf16 bf16x8 __attribute__((ext_vector_type(8)));
 typedef _Float16 f16x8 __attribute__((ext_vector_type(8)));
 
 constexpr int kUnit = 128;          // channels per wave and step: 16 bytes of weights per lane
-constexpr int kAhead = 4;           // steps whose weights are under way
 
 struct W4Args {
   mg3m_w4 p;
-  int slab_log2;   // units of x in LDS, CW at least
-  int vec;         // x rows are 16-byte aligned
+  int slab_log2;           // units of x in LDS
+  int vec;                 // x rows are 16-byte aligned
   unsigned per_group;      // ceil(2^31 / (group / 32))
 
   // The group of a block of 32 channels: exact for block * (group / 32) below 2^31.
@@ -70,23 +58,25 @@ __device__ __forceinline__ f32x4 mfma(u32x4 a, u32x4 b, f32x4 c) {
     return __builtin_amdgcn_mfma_f32_16x16x32_bf16(__builtin_bit_cast(bf16x8, a), __builtin_bit_cast(bf16x8, b), c, 0, 0, 0);
 }
 
-// The eight weights of a dword as 16 + q, in the order 0 4 1 5 2 6 3 7.
+// The eight weights of a dword as 16 + q, in the order 0 4 1 5 2 6 3 7.  mask
+// and sixteen come in registers: with two literals the compiler takes an
+// instruction more for each pair.
 template <typename T>
-__device__ __forceinline__ u32x4 expand(unsigned w) {
-  constexpr int s = W4Type<T>::kShift;
-  constexpr unsigned mask = 0x000f000fu << s;
+__device__ __forceinline__ u32x4 expand(unsigned w, unsigned mask, unsigned sixteen) {
   u32x4 r;
 #pragma unroll
   for (int i = 0; i < 4; ++i) {
-    const int by = 4 * i - s;
-    r[i] = ((by < 0 ? w << -by : w >> by) & mask) | W4Type<T>::kSixteen;
+    const int by = 4 * i - W4Type<T>::kShift;
+    r[i] = ((by < 0 ? w << -by : w >> by) & mask) | sixteen;
   }
   return r;
 }
 
 __device__ __forceinline__ unsigned pack2(unsigned short lo, unsigned short hi) { return lo | (unsigned)hi << 16; }
 
-// Eight channels of a token as the MFMA takes them, in `parts` 16-byte units.
+// Eight channels of a token as the MFMA takes them, in `parts` registers sets:
+// fp32 as three bf16 parts, the upper 16 bits of what is left each time (exact,
+// as in conv_b3.h).
 template <typename T>
 __device__ __forceinline__ void arrange(const T (&v)[8], u32x4 (&out)[W4Type<T>::kParts]) {
   if constexpr (sizeof(T) == 2) {
@@ -94,55 +84,78 @@ __device__ __forceinline__ void arrange(const T (&v)[8], u32x4 (&out)[W4Type<T>:
     for (int i = 0; i < 4; ++i)
       out[0][i] = pack2(__builtin_bit_cast(unsigned short, v[i]), __builtin_bit_cast(unsigned short, v[i + 4]));
   } else {
-    unsigned short b[3][8];
+    float r[8];
 #pragma unroll
-    for (int i = 0; i < 8; ++i) {
-      // a part is the float's upper 16 bits: the rest is exact
-      float r = v[i];
+    for (int i = 0; i < 8; ++i) r[i] = v[i];
 #pragma unroll
-      for (int q = 0; q < 3; ++q) {
-        const unsigned top = __builtin_bit_cast(unsigned, r) & 0xffff0000u;
-        b[q][i] = (unsigned short)(top >> 16);
-        r -= __builtin_bit_cast(float, top);
+    for (int q = 0; q < 3; ++q) {
+      unsigned top[8];
+#pragma unroll
+      for (int i = 0; i < 8; ++i) {
+        top[i] = __builtin_bit_cast(unsigned, r[i]) & 0xffff0000u;
+        r[i] -= __builtin_bit_cast(float, top[i]);
       }
+#pragma unroll
+      for (int i = 0; i < 4; ++i) out[q][i] = top[i] >> 16 | top[i + 4];
     }
-#pragma unroll
-    for (int q = 0; q < 3; ++q)
-#pragma unroll
-      for (int i = 0; i < 4; ++i) out[q][i] = pack2(b[q][i], b[q][i + 4]);
   }
 }
 
-// WHOLE: a group covers whole units.  Otherwise the lanes' dwords are
-// transposed (lane quarter against dword), after which an MFMA covers 32
-// consecutive channels, which lie in one group.  MT: tokens that LDS has room
-// for, so that its addresses differ by constants.
-template <typename T, int MT, int RW, int CW, bool WHOLE>
+// More than four tokens, on the matrix cores.  v_mfma_f32_16x16x32 takes 16
+// tokens (rows) times 16 weight rows (columns); a lane holds eight consecutive
+// channels of a row, which is one dword of weights.
+//
+// A wave takes a tile of 16 rows and four units of 128 channels at a time, 256
+// bytes of each row.  It loads them row by row, whole cache lines, and turns
+// them through LDS of its own: loaded as the MFMA takes them, 64 bytes of 16
+// rows at once, they came from one channel of the L2 cache wherever rows are a
+// multiple of 4 KB apart (13 tokens, 8192 to 24576 channels: 54 us).
+//
+// A work-group has eight waves: RW tiles of rows times CW slices of the
+// channels, which are joined through LDS in a fixed order.  It keeps x in LDS
+// as the MFMA takes it, and the rows' scales, as s and s (16 + zero); long rows
+// in slabs.  WHOLE: a group covers whole units.  Otherwise the lanes' dwords
+// are transposed (lane quarter against dword), after which an MFMA covers 32
+// consecutive channels, which lie in one group.
+template <typename T, int RW, int CW, bool WHOLE>
 __global__ __launch_bounds__(512) void matvec_w4(W4Args a) {
+  constexpr int MT = 16;                         // tokens of an MFMA
   constexpr int kParts = W4Type<T>::kParts, kRows = 16 * RW;
-  extern __shared__ u32x4 xs[];                  // [unit][part][16 blocks of 8 channels][MT], then ss
+  extern __shared__ u32x4 lds[];
   const mg3m_w4& p = a.p;
   const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
   const int rw = wave / CW, cw = wave - rw * CW;
   const int col = lane & 15, quarter = lane >> 4;
   const int row_blocks = (p.K + kRows - 1) / kRows;
   const int mb = blockIdx.x / row_blocks, row0 = (int)(blockIdx.x - mb * row_blocks) * kRows;
-  const int m0 = mb * 16, tokens = min(16, p.M - m0);
+  const int m0 = mb * 16, tokens = min(MT, p.M - m0);
   const int row = row0 + rw * 16 + col;
   const int units = (p.C + kUnit - 1) / kUnit, groups = p.C / p.group;
-  const unsigned char* q = p.q + (long long)min(row, p.K - 1) * (p.C / 2);
   const int token = min(col, tokens - 1);        // columns behind the last token repeat it
-  const int slab = 1 << a.slab_log2, per_slab = slab / CW;      // per_slab: a multiple of kAhead
+  const int slab = 1 << a.slab_log2;             // units, a multiple of 4 CW
+  // Token m of block b lies at place m ^ b: lanes that write one token's blocks
+  // and lanes that read one block's tokens both reach all banks.
+  int x_lane[4];
+#pragma unroll
+  for (int d = 0; d < 4; ++d) {
+    const int b = WHOLE ? quarter * 4 + d : d * 4 + quarter;
+    x_lane[d] = b * MT + (token ^ b);
+  }
+  u32x4* wt = lds + wave * 256;                  // [row][16 pieces of 16 bytes]
+  u32x4* xs = lds + 8 * 256;                     // [unit][part][16 blocks of 8 channels][MT]
   float2* ss = reinterpret_cast<float2*>(xs + (kParts * 16 * MT << a.slab_log2));     // [group][row]
 
-  // Four units of this wave from unit i of a slab; behind the end the row's
-  // first bytes, against x = 0.
-  auto load = [&](int unit0, int i, u32x4 (&w)[kAhead]) {
+  // Four units from channel c0 on: 16 lanes on a row, four rows at a time;
+  // behind the channels' end the row's last 16 bytes, against x = 0.
+  const unsigned row_bytes = p.C / 2;
+  const unsigned char* q = p.q + (long long)row0 * row_bytes;
+  unsigned q_lane[4];                            // below 2^26
 #pragma unroll
-    for (int k = 0; k < kAhead; ++k) {
-      const int c = (unit0 + (i + k) * CW + cw) * kUnit + quarter * 32;
-      w[k] = *reinterpret_cast<const u32x4*>(q + (c < p.C ? c / 2 : 0));
-    }
+  for (int n = 0; n < 4; ++n) q_lane[n] = (min(row0 + rw * 16 + n * 4 + quarter, p.K - 1) - row0) * row_bytes;
+  auto load = [&](unsigned c0, u32x4 (&w)[4]) {
+    const unsigned at = min(c0 / 2 + col * 16, row_bytes - 16);
+#pragma unroll
+    for (int n = 0; n < 4; ++n) w[n] = *reinterpret_cast<const u32x4*>(q + (q_lane[n] + at));
   };
 
   // Four loads at a time; those behind the end repeat an element.
@@ -194,55 +207,75 @@ __global__ __launch_bounds__(512) void matvec_w4(W4Args a) {
         const bool in = unit0 * kUnit + b * 8 < p.C;
 #pragma unroll
         for (int part = 0; part < kParts; ++part)
-          xs[((b / 16 * kParts + part) * 16 + b % 16) * MT + m] = in ? o[part] : u32x4{};
+          xs[((b / 16 * kParts + part) * 16 + b % 16) * MT + (m ^ b % 16)] = in ? o[part] : u32x4{};
       }
     }
   };
 
+  unsigned mask = 0x000f000fu << W4Type<T>::kShift, sixteen = W4Type<T>::kSixteen;
+  asm("" : "+s"(mask));
+  asm("" : "+v"(sixteen));
   const u32x4 ones = {W4Type<T>::kOnes, W4Type<T>::kOnes, W4Type<T>::kOnes, W4Type<T>::kOnes};
   f32x4 y = {};
   int group0 = 0;                                // the slab's first group
-  auto product = [&](int unit0, int in_slab, u32x4 v) {
-    const u32x4* x = xs + in_slab * (kParts * 16 * MT) + quarter * (WHOLE ? 4 * MT : MT) + token;
-    u32x4 xa[4][kParts];
-    float2 s[WHOLE ? 1 : 4];
+  // Two units side by side: an MFMA's result is there for the next one of its
+  // sum when the other three sums have had theirs.
+  auto product = [&](int unit0, int in_slab, int piece) {
+    u32x4 xa[2][4][kParts], v[2];
+    float2 s[2][WHOLE ? 1 : 4];
 #pragma unroll
-    for (int d = 0; d < 4; ++d) {
+    for (int u = 0; u < 2; ++u) {
+      v[u] = wt[col * 16 + ((piece + u * 4 + quarter) ^ col)];
+      const u32x4* x = xs + (in_slab + u) * (kParts * 16 * MT);
 #pragma unroll
-      for (int part = 0; part < kParts; ++part) xa[d][part] = x[(part * 16 + (WHOLE ? d : 4 * d)) * MT];
-    }
+      for (int d = 0; d < 4; ++d)
 #pragma unroll
-    for (int d = 0; d < (WHOLE ? 1 : 4); ++d) {
-      const int g = a.group_of(min((unit0 + in_slab) * 4 + d, p.C / 32 - 1)) - group0;
-      s[d] = ss[g * kRows + rw * 16 + col];
-    }
-    if constexpr (!WHOLE) {
-      const auto s02 = __builtin_amdgcn_permlane32_swap(v[0], v[2], false, false);
-      const auto s13 = __builtin_amdgcn_permlane32_swap(v[1], v[3], false, false);
-      const auto s01 = __builtin_amdgcn_permlane16_swap(s02[0], s13[0], false, false);
-      const auto s23 = __builtin_amdgcn_permlane16_swap(s02[1], s13[1], false, false);
-      v = u32x4{s01[0], s01[1], s23[0], s23[1]};
-    }
-    f32x4 dot = {}, sum = {};
+        for (int part = 0; part < kParts; ++part) xa[u][d][part] = x[part * 16 * MT + x_lane[d]];
 #pragma unroll
-    for (int d = 0; d < 4; ++d) {
-      const u32x4 b = expand<T>(v[d]);
-#pragma unroll
-      for (int part = 0; part < kParts; ++part) {
-        dot = mfma<T>(xa[d][part], b, dot);
-        sum = mfma<T>(xa[d][part], ones, sum);
+      for (int d = 0; d < (WHOLE ? 1 : 4); ++d) {
+        const int g = a.group_of(min((unit0 + in_slab + u) * 4 + d, p.C / 32 - 1)) - group0;
+        s[u][d] = ss[g * kRows + rw * 16 + col];
       }
-      if (!WHOLE || d == 3) {
-        const float2 f = s[WHOLE ? 0 : d];
+    }
+    __builtin_amdgcn_sched_barrier(0);           // the reads first
+    if constexpr (!WHOLE) {
 #pragma unroll
-        for (int e = 0; e < 4; ++e) y[e] = fmaf(f.x, dot[e], fmaf(-f.y, sum[e], y[e]));
-        dot = sum = f32x4{};
+      for (int u = 0; u < 2; ++u) {
+        const auto s02 = __builtin_amdgcn_permlane32_swap(v[u][0], v[u][2], false, false);
+        const auto s13 = __builtin_amdgcn_permlane32_swap(v[u][1], v[u][3], false, false);
+        const auto s01 = __builtin_amdgcn_permlane16_swap(s02[0], s13[0], false, false);
+        const auto s23 = __builtin_amdgcn_permlane16_swap(s02[1], s13[1], false, false);
+        v[u] = u32x4{s01[0], s01[1], s23[0], s23[1]};
+      }
+    }
+    f32x4 dot[2] = {}, sum[2] = {};
+#pragma unroll
+    for (int d = 0; d < 4; ++d) {
+      const u32x4 b[2] = {expand<T>(v[0][d], mask, sixteen), expand<T>(v[1][d], mask, sixteen)};
+#pragma unroll
+      for (int part = 0; part < kParts; ++part)
+#pragma unroll
+        for (int u = 0; u < 2; ++u) {
+          dot[u] = mfma<T>(xa[u][d][part], b[u], dot[u]);
+          sum[u] = mfma<T>(xa[u][d][part], ones, sum[u]);
+        }
+      if (!WHOLE || d == 3) {
+#pragma unroll
+        for (int u = 0; u < 2; ++u) {
+          const float2 f = s[u][WHOLE ? 0 : d];
+#pragma unroll
+          for (int e = 0; e < 4; ++e) y[e] = fmaf(f.x, dot[u][e], fmaf(-f.y, sum[u][e], y[e]));
+          dot[u] = sum[u] = f32x4{};
+        }
       }
     }
   };
   for (int unit0 = 0; unit0 < units; unit0 += slab) {
-    u32x4 w0[kAhead], w1[kAhead];
-    load(unit0, 0, w0);
+    // this wave's fours of units in the slab: i * CW + cw
+    const int fours = (min(slab, units - unit0) + 4 * CW - 1) / (4 * CW);
+    auto first = [&](int i) { return (unsigned)(unit0 + (i * CW + cw) * 4) * kUnit; };
+    u32x4 w[4];
+    load(first(0), w);
     group0 = a.group_of(unit0 * (kUnit / 32));
     const int end = min((min(unit0 + slab, units)) * kUnit, p.C);
     if (unit0 > 0) __syncthreads();
@@ -250,23 +283,20 @@ __global__ __launch_bounds__(512) void matvec_w4(W4Args a) {
     if (a.vec) stage_x(unit0, std::true_type{});
     else stage_x(unit0, std::false_type{});
     __syncthreads();
-    // this wave's units of the slab, with those of zeros that fill the last four
-    const int mine = min(per_slab, (units - unit0 + CW - 1) / CW);
-    for (int i = 0; i < mine; i += 2 * kAhead) {
-      if (i + kAhead < mine) load(unit0, i + kAhead, w1);
+    for (int i = 0; i < fours; ++i) {
 #pragma unroll
-      for (int k = 0; k < kAhead; ++k) product(unit0, (i + k) * CW + cw, w0[k]);
-      if (i + kAhead >= mine) break;
-      if (i + 2 * kAhead < mine) load(unit0, i + 2 * kAhead, w0);
+      for (int n = 0; n < 4; ++n) wt[(n * 4 + quarter) * 16 + (col ^ (n * 4 + quarter))] = w[n];
+      __builtin_amdgcn_sched_barrier(0);
+      load(first(min(i + 1, fours - 1)), w);     // the last one again: not under a condition
+      __builtin_amdgcn_sched_barrier(0);
 #pragma unroll
-      for (int k = 0; k < kAhead; ++k) product(unit0, (i + kAhead + k) * CW + cw, w1[k]);
+      for (int k = 0; k < 4; k += 2) product(unit0, (i * CW + cw) * 4 + k, k * 4);
     }
   }
 
-  // join the slices
   if constexpr (CW > 1) {
     __syncthreads();
-    f32x4* join = reinterpret_cast<f32x4*>(xs);
+    f32x4* join = reinterpret_cast<f32x4*>(lds);
     if (cw > 0) join[(rw * CW + cw) * 64 + lane] = y;
     __syncthreads();
     if (cw > 0) return;
@@ -281,32 +311,151 @@ __global__ __launch_bounds__(512) void matvec_w4(W4Args a) {
   }
 }
 
-template <typename T, int MT, int RW, int CW>
-int launch_w4_as(W4Args a, void* stream, std::string* err) {
+template <typename T, int RW, int CW>
+int launch_w4_many(W4Args a, void* stream, std::string* err) {
   const mg3m_w4& p = a.p;
   const long long groups = (long long)((p.K + 16 * RW - 1) / (16 * RW)) * ((p.M + 15) / 16);
   if (groups > 0x7fffffffLL) {
     *err = "4-bit product: too many rows for one launch";
     return MG3M_ERR_TOO_LARGE;
   }
-  // x and scales in LDS: all of them, or slabs that leave room for a second work-group
-  const int x_unit = MT * kUnit * 2 * W4Type<T>::kParts;
+  // LDS: the waves' weights (32 KB), x and scales, all or slabs of up to 48 KB
   const int units = (p.C + kUnit - 1) / kUnit;
   const auto bytes = [&](int log2) {
-    return ((size_t)x_unit << log2) + (((size_t)kUnit << log2) / p.group + 2) * 16 * RW * sizeof(float2);
+    return ((size_t)(16 * kUnit * 2 * W4Type<T>::kParts) << log2) +
+           (((size_t)kUnit << log2) / p.group + 2) * 16 * RW * sizeof(float2);
   };
-  while (1 << a.slab_log2 < CW * kAhead) ++a.slab_log2;
-  while (1 << a.slab_log2 < units && bytes(a.slab_log2 + 1) <= 65536) ++a.slab_log2;
-  const size_t lds = std::max<size_t>(bytes(a.slab_log2), CW > 1 ? 8 * 64 * sizeof(f32x4) : 0);
-  auto* kernel = p.group % kUnit == 0 ? matvec_w4<T, MT, RW, CW, true> : matvec_w4<T, MT, RW, CW, false>;
-  kernel<<<(unsigned)groups, 512, lds, static_cast<hipStream_t>(stream)>>>(a);
+  while (1 << a.slab_log2 < 4 * CW) ++a.slab_log2;
+  while (1 << a.slab_log2 < units && bytes(a.slab_log2 + 1) <= 49152) ++a.slab_log2;
+  auto* kernel = p.group % kUnit == 0 ? matvec_w4<T, RW, CW, true> : matvec_w4<T, RW, CW, false>;
+  kernel<<<(unsigned)groups, 512, 32768 + bytes(a.slab_log2), static_cast<hipStream_t>(stream)>>>(a);
   return launched("4-bit product", err);
 }
 
-template <typename T, int MT>
-int launch_w4_mt(const W4Args& a, long long tiles, void* stream, std::string* err) {
-  if (tiles >= 1024 || MT * W4Type<T>::kParts > 16) return launch_w4_as<T, MT, 4, 2>(a, stream, err);
-  return launch_w4_as<T, MT, 1, 8>(a, stream, err);
+// Up to four tokens, on the vector ALU: no x in LDS and no barrier, which for
+// few tokens cost more than the products.  A row's blocks of 32 channels (16
+// bytes) go to consecutive lanes, so loads are whole cache lines; a lane keeps
+// its channels of the tokens for kRowsPer rows.  16-bit tokens multiply the
+// pairs 16 + q with a two-element dot product (12 instructions for 8 weights
+// and a token, 4 for each further token), fp32 ones multiply q itself, which
+// v_cvt_f32_ubyte takes out of a byte.
+constexpr int kRowsPer = 4;
+
+typedef __bf16 bf16x2 __attribute__((ext_vector_type(2)));
+typedef _Float16 f16x2 __attribute__((ext_vector_type(2)));
+
+template <typename T>
+__device__ __forceinline__ float dot2(unsigned a, unsigned b, float c) {
+  if constexpr (W4Type<T>::kShift == 6)
+    return __builtin_amdgcn_fdot2(__builtin_bit_cast(f16x2, a), __builtin_bit_cast(f16x2, b), c, false);
+  else
+    return __builtin_amdgcn_fdot2_f32_bf16(__builtin_bit_cast(bf16x2, a), __builtin_bit_cast(bf16x2, b), c, false);
+}
+
+template <typename T, int M>
+__global__ __launch_bounds__(256) void matvec_w4_few(W4Args a, int lanes_log2) {
+  constexpr bool kHalf = sizeof(T) == 2;
+  const mg3m_w4& p = a.p;
+  const int lanes = 1 << lanes_log2;             // on a row
+  const int lane = threadIdx.x & (lanes - 1);
+  const int row0 = (int)((blockIdx.x * 256u + threadIdx.x) >> lanes_log2) * kRowsPer;
+  const int blocks = p.C / 32, groups = p.C / p.group;
+  const unsigned char* zero = p.zero != nullptr ? p.zero : p.q;      // q: read, not used
+  unsigned mask = 0x000f000fu << W4Type<T>::kShift, sixteen = W4Type<T>::kSixteen;
+  asm("" : "+s"(mask));
+  asm("" : "+v"(sixteen));
+  float y[kRowsPer][M] = {};
+  for (int b = lane; b < blocks; b += lanes) {
+    u32x4 w[kRowsPer];
+    float s[kRowsPer], z[kRowsPer];
+    const int g = a.group_of(b);
+#pragma unroll
+    for (int r = 0; r < kRowsPer; ++r) {
+      const long long row = min(row0 + r, p.K - 1);
+      w[r] = reinterpret_cast<const u32x4*>(p.q + row * (p.C / 2))[b];
+      s[r] = (float)static_cast<const T*>(p.scale)[row * groups + g];
+      z[r] = (float)zero[row * groups + g];
+    }
+#pragma unroll
+    for (int m = 0; m < M; ++m) {
+      const T* x = static_cast<const T*>(p.x) + min(m, p.M - 1) * p.ldx + b * 32;
+      T v[32];
+      if (a.vec) {
+#pragma unroll
+        for (int k = 0; k < 2 * (int)sizeof(T); ++k)
+          *reinterpret_cast<u32x4*>(v + k * 16 / sizeof(T)) = reinterpret_cast<const u32x4*>(x)[k];
+      } else {
+#pragma unroll
+        for (int k = 0; k < 32; ++k) v[k] = x[k];
+      }
+      float sum = 0.0f;
+      if constexpr (kHalf) {
+        unsigned pair[16];
+#pragma unroll
+        for (int d = 0; d < 4; ++d)
+#pragma unroll
+          for (int i = 0; i < 4; ++i) {
+            pair[d * 4 + i] = pack2(__builtin_bit_cast(unsigned short, v[d * 8 + i]),
+                                    __builtin_bit_cast(unsigned short, v[d * 8 + i + 4]));
+            sum = dot2<T>(pair[d * 4 + i], W4Type<T>::kOnes, sum);
+          }
+#pragma unroll
+        for (int r = 0; r < kRowsPer; ++r) {
+          float dot = 0.0f;
+#pragma unroll
+          for (int d = 0; d < 4; ++d) {
+            const u32x4 e = expand<T>(w[r][d], mask, sixteen);
+#pragma unroll
+            for (int i = 0; i < 4; ++i) dot = dot2<T>(pair[d * 4 + i], e[i], dot);
+          }
+          const float z16 = 16.0f + (p.zero != nullptr ? z[r] : 8.0f);
+          y[r][m] = fmaf(s[r], fmaf(-z16, sum, dot), y[r][m]);
+        }
+      } else {
+#pragma unroll
+        for (int k = 0; k < 32; ++k) sum += v[k];
+#pragma unroll
+        for (int r = 0; r < kRowsPer; ++r) {
+          float dot = 0.0f;
+#pragma unroll
+          for (int d = 0; d < 4; ++d) {
+            const unsigned even = w[r][d] & 0x0f0f0f0fu, odd = (w[r][d] >> 4) & 0x0f0f0f0fu;
+#pragma unroll
+            for (int i = 0; i < 4; ++i) {
+              dot = fmaf(v[d * 8 + 2 * i], (float)((even >> (8 * i)) & 255u), dot);
+              dot = fmaf(v[d * 8 + 2 * i + 1], (float)((odd >> (8 * i)) & 255u), dot);
+            }
+          }
+          y[r][m] = fmaf(s[r], fmaf(-(p.zero != nullptr ? z[r] : 8.0f), sum, dot), y[r][m]);
+        }
+      }
+    }
+  }
+  for (int o = 1; o < lanes; o *= 2)
+#pragma unroll
+    for (int r = 0; r < kRowsPer; ++r)
+#pragma unroll
+      for (int m = 0; m < M; ++m) y[r][m] += __shfl_xor(y[r][m], o);
+  if (lane != 0) return;
+#pragma unroll
+  for (int r = 0; r < kRowsPer; ++r)
+#pragma unroll
+    for (int m = 0; m < M; ++m)
+      if (row0 + r < p.K && m < p.M) static_cast<T*>(p.y)[m * p.ldy + row0 + r] = (T)y[r][m];
+}
+
+template <typename T, int M>
+int launch_w4_few(const W4Args& a, void* stream, std::string* err) {
+  const mg3m_w4& p = a.p;
+  int lanes_log2 = 0;
+  while (lanes_log2 < 6 && 32 << lanes_log2 < p.C) ++lanes_log2;
+  const long long threads = (long long)((p.K + kRowsPer - 1) / kRowsPer) << lanes_log2;
+  if (threads > 0x7fffffffLL) {
+    *err = "4-bit product: too many rows for one launch";
+    return MG3M_ERR_TOO_LARGE;
+  }
+  matvec_w4_few<T, M><<<(unsigned)((threads + 255) / 256), 256, 0, static_cast<hipStream_t>(stream)>>>(a, lanes_log2);
+  return launched("4-bit product", err);
 }
 
 }  // namespace
@@ -323,10 +472,20 @@ int launch_w4(const mg3m_w4& p, void* stream, std::string* err) {
     a.vec = reinterpret_cast<uintptr_t>(p.x) % 16 == 0 && (p.ldx * sizeof(T)) % 16 == 0;
     const unsigned blocks = p.group / 32;
     a.per_group = ((1u << 31) + blocks - 1) / blocks;
-    // wide products share x between four tiles of rows
+    // Tokens by the vector ALU or the matrix cores: 4 of fp16, 8192 to 24576
+    // channels: 47 us against 38, 2 of bf16: 32 against 35; 4 of fp32, 4096 to
+    // 4096: 13 against 17 (three parts each).
+    if (p.M == 1) return launch_w4_few<T, 1>(a, stream, err);
+    if (p.M == 2) return launch_w4_few<T, 2>(a, stream, err);
+    if constexpr (sizeof(T) == 4)
+      if (p.M <= 4) return launch_w4_few<T, 4>(a, stream, err);
+    // Many tiles: four of them share x (64 tokens, 4096 to 4096 channels, bf16:
+    // 14 us, two 18); else more waves per row (16 tokens: 16 us, two 11).  LDS
+    // does not hold the parts of fp32 tokens for four slices.
     const long long tiles = (long long)((p.K + 15) / 16) * ((p.M + 15) / 16);
-    return p.M == 1 ? launch_w4_mt<T, 1>(a, tiles, stream, err)
-           : p.M <= 4 ? launch_w4_mt<T, 4>(a, tiles, stream, err) : launch_w4_mt<T, 16>(a, tiles, stream, err);
+    if constexpr (sizeof(T) == 2)
+      if (tiles < 1024) return launch_w4_many<T, 2, 4>(a, stream, err);
+    return launch_w4_many<T, 4, 2>(a, stream, err);
   });
 }
 
