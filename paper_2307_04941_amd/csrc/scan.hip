@@ -98,12 +98,23 @@ __global__ __launch_bounds__(256) void scan_join(ScanArgs a) {
   float* slot = a.slots + (id0 * p.S + s) * p.D + d;
   const float* sum = a.sums + id0 * p.D + d;
   const long long step = (long long)p.S * p.D;
-  for (int k = 0; k + 1 < pieces; ++k) {
-    const float end = slot[k * step];
-    slot[k * step] = h;
-    h = fmaf(__builtin_amdgcn_exp2f(A * sum[(long long)k * p.D]), h, end);
+  // Eight pieces' loads at once (16 pieces one after the other: 7.3 us, so:
+  // 4.2); those behind the last repeat it and are not used.
+  constexpr int kAt = 8;
+  for (int k0 = 0; k0 < pieces; k0 += kAt) {
+    float end[kAt], left[kAt];
+#pragma unroll
+    for (int j = 0; j < kAt; ++j) {
+      const int k = min(k0 + j, pieces - 1);
+      end[j] = slot[k * step];
+      left[j] = sum[(long long)k * p.D];
+    }
+#pragma unroll
+    for (int j = 0; j < kAt; ++j) {
+      if (k0 + j < pieces) slot[(k0 + j) * step] = h;
+      h = fmaf(__builtin_amdgcn_exp2f(A * left[j]), h, end[j]);
+    }
   }
-  slot[(pieces - 1) * step] = h;
 }
 
 ScanFn kernel_of(int dtype, const ScanPlan& s, bool ends) {

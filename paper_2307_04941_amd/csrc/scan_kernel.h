@@ -19,6 +19,8 @@
 // four waves).
 #pragma once
 
+#include <type_traits>
+
 #include "scan.h"
 
 namespace mg3m {
@@ -48,9 +50,12 @@ __global__ __launch_bounds__(64 * F) void scan_pieces(ScanArgs a) {
   const int cblocks = a.blocks * p.G;
   const int id = blockIdx.x / cblocks, cb = blockIdx.x - id * cblocks;
   const int g = cb / a.blocks, per = p.D / p.G;
-  const int in_group = (cb - g * a.blocks) * 64 + lane;
-  const bool live = in_group < per;
-  const int d = g * per + min(in_group, per - 1);
+  // channels d0 + l: d0 is the same for all lanes, so that addresses are a
+  // scalar and the lane's offset; lanes behind the group repeat its last channel
+  const int in_group = (cb - g * a.blocks) * 64, d0 = g * per + in_group;
+  const bool live = in_group + lane < per;
+  const unsigned l = min(lane, per - 1 - in_group), lb = l * sizeof(T);
+  const int d = d0 + l;
 
   Piece pc = find_piece(p.begin, p.end, p.N, p.T, a.W, id);
   const int n = __builtin_amdgcn_readfirstlane(pc.n);
@@ -74,21 +79,25 @@ __global__ __launch_bounds__(64 * F) void scan_pieces(ScanArgs a) {
   const float bias = p.dt_bias != nullptr ? p.dt_bias[d] : 0.0f;
   const float skip = !ENDS && p.D_skip != nullptr ? p.D_skip[d] : 0.0f;
 
-  const T* u = static_cast<const T*>(p.u) + (long long)b * p.ldu + d;
-  const T* dt = static_cast<const T*>(p.dt) + (long long)b * p.lddt + d;
+  const T* u = static_cast<const T*>(p.u) + (long long)b * p.ldu + d0;
+  const T* dt = static_cast<const T*>(p.dt) + (long long)b * p.lddt + d0;
   // without a gate u stands in for z and is not used: no branch per token
   const bool gate = p.z != nullptr;
-  const T* z = gate ? static_cast<const T*>(p.z) + (long long)b * p.ldz + d : u;
+  const T* z = gate ? static_cast<const T*>(p.z) + (long long)b * p.ldz + d0 : u;
   const unsigned ldu = p.ldu, lddt = p.lddt, ldz = gate ? p.ldz : p.ldu, ldy = p.ldy;
-  T* y = static_cast<T*>(p.y) + (long long)b * p.ldy + d;
+  T* y = static_cast<T*>(p.y) + (long long)b * p.ldy + d0;
   const float* bc = a.bc + (((long long)g * F + f) * p.T + b) * (2 * P);
 
   // rows and distances are below 2^31: one 32 x 32 bit product per address
   auto row_at = [](int row, unsigned ld) { return (unsigned long long)(unsigned)row * ld; };
+  using Raw = std::conditional_t<sizeof(T) == 4, unsigned, unsigned short>;
   // this wave's tokens of a tile; those behind the end read the last token
   auto load = [&](const T* x, unsigned ld, int tile, unsigned (&v)[kOwn]) {
 #pragma unroll
-    for (int k = 0; k < kOwn; ++k) v[k] = raw_load(x + row_at(min(tile * kTile + f + k * F, tokens - 1), ld));
+    for (int k = 0; k < kOwn; ++k) {
+      const T* row = x + row_at(min(tile * kTile + f + k * F, tokens - 1), ld);
+      v[k] = *reinterpret_cast<const Raw*>(reinterpret_cast<const char*>(row) + lb);
+    }
   };
   auto step_size = [&](unsigned raw) {
     const float v = raw_value<T>(raw) + bias;
@@ -105,7 +114,7 @@ __global__ __launch_bounds__(64 * F) void scan_pieces(ScanArgs a) {
 #pragma unroll
     for (int k = 0; k < kOwn; ++k) {
       const int t = tile * kTile + f + k * F;
-      if (live && t < tokens) y[row_at(t, ldy)] = (T)out[k];
+      if (live && t < tokens) *reinterpret_cast<T*>(reinterpret_cast<char*>(y + row_at(t, ldy)) + lb) = (T)out[k];
     }
   };
 

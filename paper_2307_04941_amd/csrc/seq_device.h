@@ -21,14 +21,9 @@ int with_dtype(int dtype, F&& f) {
   }
 }
 
-// An element as loaded, in 32 bits.  The empty asm keeps the compiler from
-// holding it in 16 across a loop, which takes an instruction after the load
-// and so a wait for it.
-template <typename T>
-__device__ __forceinline__ unsigned raw_load(const T* p) {
-  if constexpr (sizeof(T) == 4) return *reinterpret_cast<const unsigned*>(p);
-  else return *reinterpret_cast<const unsigned short*>(p);
-}
+// The value of an element loaded into 32 bits.  The empty asm keeps the
+// compiler from holding it in 16 across a loop, which takes an instruction
+// after the load and so a wait for it.
 template <typename T>
 __device__ __forceinline__ float raw_value(unsigned v) {
   if constexpr (sizeof(T) == 4) {
@@ -120,15 +115,15 @@ __device__ __forceinline__ float sigmoid(float v) {
 }
 
 // log(1 + exp(v)) = max(v, 0) + log(1 + e), e = exp(-|v|) in (0, 1].  1 + e
-// rounds to w; log(w) * e / (w - 1) is log(1 + e) to a few roundings for any e
-// (Kahan's correction: log(1 + e) / e is flat where w - 1 differs from e), so
-// steps far below 2^-24 keep their relative precision.
+// rounds to w and leaves r = e - (w - 1), exactly, so log(1 + e) = log(w) +
+// log(1 + r / w); r is at most 2^-24 and r / w differs from r by less than a
+// rounding of the result.  Steps far below 2^-24 keep their precision: w is 1
+// and r is e.
 __device__ __forceinline__ float softplus(float v) {
   const float e = __builtin_amdgcn_exp2f(-fabsf(v) * kLog2e);
   const float w = 1.0f + e;
-  const float d = w - 1.0f;
-  const float l = d == 0.0f ? e : __builtin_amdgcn_logf(w) * kLn2 * (e * __builtin_amdgcn_rcpf(d));
-  return fmaxf(v, 0.0f) + l;
+  const float r = e - (w - 1.0f);
+  return fmaxf(v, 0.0f) + fmaf(__builtin_amdgcn_logf(w), kLn2, r);
 }
 
 }  // namespace mg3m

@@ -586,6 +586,9 @@ def _row_distance(t, name, tail=1):
     `tail` sizes are a row, dense; the leading ones count rows that lie at one
     distance."""
     shape, strides, width = t.shape, t.stride(), 1
+    # the usual case: rows of one leading size, more than one of them
+    if strides[-1] == 1 and shape[0] > 1 and len(shape) == tail + 1 and (tail == 1 or strides[1] == shape[2]):
+        return strides[0]
     for i in range(len(shape) - 1, len(shape) - 1 - tail, -1):
         if shape[i] != 1 and strides[i] != width:
             raise ValueError(f"the channels of {name} must be contiguous")
