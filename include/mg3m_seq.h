@@ -37,7 +37,9 @@
  * or a begin without an end; MG3M_ERR_ALIGN for a pointer not aligned to its
  * element; MG3M_ERR_ALIAS if an output (y, state) shares an element with any
  * other tensor, where rows of one distance that interleave without sharing an
- * element are accepted.  Tensors may exceed 4 GiB.
+ * element are accepted; MG3M_ERR_TOO_LARGE for T above 2^31 - 2^16, C (of the
+ * convolution), M, K or D * S above 2^30, C of the 4-bit product above 2^20, or
+ * more work-groups than a launch takes.  Tensors may exceed 4 GiB.
  */
 #ifndef MG3M_SEQ_H
 #define MG3M_SEQ_H
@@ -127,7 +129,9 @@ int selective_scan_step(const mg3m_scan *a, void *stream);
  * q: [K][C/2] bytes, the even c in the low four bits, values 0..15 (16-byte
  * aligned); scale: [K][C/group] of the type of x; zero: [K][C/group] bytes,
  * or NULL for 8.  group is a multiple of 32 that divides C.  Made for few
- * tokens: each 16 tokens read the weights once. */
+ * tokens: each 16 tokens read the weights once.  A token with an infinity or a
+ * NaN gives NaN or infinities in its own row; fp32 channels below 2^-100 lose
+ * low bits. */
 typedef struct mg3m_w4 {
     const void *x;            /* [M][C], distance ldx */
     const unsigned char *q;

@@ -31,7 +31,6 @@ struct W4Args {
   // The group of a block of 32 channels: exact for block * (group / 32) below 2^31.
   __device__ __forceinline__ int group_of(int block) const { return (int)__umulhi(2u * block, per_group); }
 };
-constexpr int kMaxChannels = 1 << 20;
 
 template <typename T>
 struct W4Type;
@@ -461,10 +460,6 @@ int launch_w4_few(const W4Args& a, void* stream, std::string* err) {
 }  // namespace
 
 int launch_w4(const mg3m_w4& p, void* stream, std::string* err) {
-  if (p.C > kMaxChannels) {
-    *err = "4-bit product: more than 2^20 channels";
-    return MG3M_ERR_TOO_LARGE;
-  }
   return with_dtype(p.dtype, [&](auto t) {
     using T = decltype(t);
     W4Args a{};

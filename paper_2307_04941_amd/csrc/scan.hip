@@ -91,7 +91,7 @@ __global__ __launch_bounds__(256) void scan_join(ScanArgs a) {
   if (i >= p.D * p.S) return;
   const int s = i / p.D, d = i - s * p.D;
   const SeqRange r = seq_range(p.begin, p.end, n, p.N, p.T);
-  const int pieces = max(1, (r.e - r.b + a.W - 1) / a.W);
+  const int pieces = max(1, ceil_div(r.e - r.b, a.W));
   const long long id0 = p.begin == nullptr ? (long long)n * pieces : piece_base(p.begin, n, p.T, a.W);
   const float A = p.A[(long long)d * p.S + s] * kLog2e;
   float h = p.load_state ? p.state[((long long)n * p.D + d) * p.S + s] : 0.0f;
@@ -129,14 +129,14 @@ ScanFn kernel_of(int dtype, const ScanPlan& s, bool ends) {
 // the next power of two of S / 4 lanes, which then sum its output.  Bound by
 // the states' bytes.
 template <typename T, bool VEC>
-__global__ __launch_bounds__(256) void scan_token(mg3m_scan p, int lanes_log2) {
-  const long long i = (long long)blockIdx.x * 256 + threadIdx.x;
-  const int lanes = 1 << lanes_log2, q = (int)(i & (lanes - 1));
-  long long row = i >> lanes_log2;                  // sequence and channel
-  const bool live = row < (long long)p.N * p.D;
-  if (!live) row = 0;
-  const int n = (int)(row / p.D), d = (int)(row - (long long)n * p.D), s0 = 4 * q;
-  const int g = d / (p.D / p.G);
+__global__ __launch_bounds__(256) void scan_token(mg3m_scan p, int lanes_log2, int blocks) {
+  const int n = blockIdx.x / blocks;                // the same for all lanes
+  const int i = (int)(blockIdx.x - n * blocks) * 256 + threadIdx.x;
+  const int lanes = 1 << lanes_log2, q = i & (lanes - 1);
+  const bool live = i >> lanes_log2 < p.D;
+  const int d = min(i >> lanes_log2, p.D - 1), s0 = 4 * q;
+  const int g = p.G == 1 ? 0 : d / (p.D / p.G);
+  const long long row = (long long)n * p.D + d;
   float* state = p.state + row * p.S + s0;
   const float* rate = p.A + (long long)d * p.S + s0;
   const T* B = static_cast<const T*>(p.B) + n * p.ldb + g * p.S + s0;
@@ -222,7 +222,7 @@ int launch_scan(const mg3m_scan& p, void* ws, void* stream, std::string* err) {
   a.blocks = (p.D / p.G + 63) / 64;
   const long long groups = piece_count(p.begin, p.N, p.T, s.W) * p.G * a.blocks;
   const long long pack = ((long long)p.G * s.F * p.T * 2 * s.P + 255) / 256;
-  if (groups > 0x7fffffffLL || pack > 0x7fffffffLL || p.N > 65535) {
+  if (groups > 0x7fffffffLL || pack > 0x7fffffffLL || (s.W != 0 && p.N > 65535)) {
     *err = "selective scan: too many rows, sequences or channels for one launch";
     return MG3M_ERR_TOO_LARGE;
   }
@@ -248,7 +248,7 @@ int launch_scan(const mg3m_scan& p, void* ws, void* stream, std::string* err) {
 int launch_scan_step(const mg3m_scan& p, void* stream, std::string* err) {
   int lanes_log2 = 0;
   while (4 << lanes_log2 < p.S) ++lanes_log2;
-  const long long groups = (((long long)p.N * p.D << lanes_log2) + 255) / 256;
+  const long long blocks = (((long long)p.D << lanes_log2) + 255) / 256, groups = blocks * p.N;
   if (groups > 0x7fffffffLL) {
     *err = "selective scan: too many sequences and channels for one launch";
     return MG3M_ERR_TOO_LARGE;
@@ -257,7 +257,7 @@ int launch_scan_step(const mg3m_scan& p, void* stream, std::string* err) {
   return with_dtype(p.dtype, [&](auto t) {
     using T = decltype(t);
     auto* kernel = vec ? scan_token<T, true> : scan_token<T, false>;
-    kernel<<<(unsigned)groups, 256, 0, static_cast<hipStream_t>(stream)>>>(p, lanes_log2);
+    kernel<<<(unsigned)groups, 256, 0, static_cast<hipStream_t>(stream)>>>(p, lanes_log2, (int)blocks);
     return launched("selective scan", err);
   });
 }

@@ -62,7 +62,7 @@ __global__ __launch_bounds__(64 * F) void scan_pieces(ScanArgs a) {
   const bool last = __builtin_amdgcn_readfirstlane((int)pc.last);
   if (n < 0 || (ENDS && last)) return;
   const int b = __builtin_amdgcn_readfirstlane(pc.b), e = __builtin_amdgcn_readfirstlane(pc.e);
-  const int tokens = e - b, tiles = (tokens + kTile - 1) / kTile;
+  const int tokens = e - b, tiles = ceil_div(tokens, kTile);
 
   // states f * P .. + P of channel d
   float A[P], h[P];

@@ -26,6 +26,8 @@ struct Rows {
 
 // Sizes are ints and distances at most 2^30 elements, so extents fit 64 bits.
 constexpr long long kMaxDistance = 1LL << 30;
+// Rows, and what else the kernels count in ints, stay clear of their end.
+constexpr int kMaxRows = 0x7fff0000, kMaxSize = 1 << 30;
 
 Rows dense(const char* name, const void* p, long long n, int size, bool out = false) {
   return {name, p, 1, n, n, size, out};
@@ -52,7 +54,7 @@ int check_rows(std::initializer_list<Rows> ts) {
     if (t.first() % t.size != 0)
       return set_error(MG3M_ERR_ALIGN, std::string(t.name) + " is not aligned to its " + std::to_string(t.size) +
                                            "-byte elements");
-    if (t.ld < t.cols || t.ld > kMaxDistance)
+    if (t.ld < t.cols || (t.rows > 1 && t.ld > kMaxDistance))
       return set_error(MG3M_ERR_SHAPE, "the distance between rows of " + std::string(t.name) + " is " +
                                            std::to_string(t.ld) + ": " + std::to_string(t.cols) + " to 2^30 allowed");
   }
@@ -75,6 +77,7 @@ int check_type(int dtype) {
 int check_sequences(const int* begin, const int* end, int T, int N) {
   if (T < 0 || N < 1) return set_error(MG3M_ERR_SHAPE, "T must be >= 0 and N >= 1");
   if ((begin == nullptr) != (end == nullptr)) return set_error(MG3M_ERR_ARG, "give begin and end, or neither");
+  if (T > kMaxRows) return set_error(MG3M_ERR_TOO_LARGE, "more than 2^31 - 2^16 rows");
   if (begin == nullptr && T % N != 0)
     return set_error(MG3M_ERR_SHAPE, "T must be a multiple of N when begin and end are NULL");
   if (reinterpret_cast<uintptr_t>(begin) % 4 != 0 || reinterpret_cast<uintptr_t>(end) % 4 != 0)
@@ -99,6 +102,7 @@ int conv1d(const mg3m_conv1d* in, bool step, void* stream) {
   }
   if (int rc = check_sequences(a.begin, a.end, a.T, a.N)) return rc;
   if (a.C < 1 || a.R < 1 || a.R > 8) return set_error(MG3M_ERR_SHAPE, "C must be >= 1 and R 1..8");
+  if (a.C > kMaxSize) return set_error(MG3M_ERR_TOO_LARGE, "more than 2^30 channels");
   if (a.w == nullptr || (a.T > 0 && (a.x == nullptr || a.y == nullptr)))
     return set_error(MG3M_ERR_NULL, "x, w and y must be non-NULL");
   if (a.R == 1) a.state = nullptr;
@@ -124,7 +128,7 @@ int check_scan_sizes(int T, int D, int G, int S, int N) {
   if (T < 0 || N < 1) return set_error(MG3M_ERR_SHAPE, "T must be >= 0 and N >= 1");
   if (D < 1 || G < 1 || D % G != 0 || S < 1 || S > 256)
     return set_error(MG3M_ERR_SHAPE, "D must be >= 1, G divide it, and S be 1..256");
-  if ((long long)D * S > 0x7fffffffLL) return set_error(MG3M_ERR_TOO_LARGE, "D * S above 2^31 - 1");
+  if ((long long)D * S > kMaxSize) return set_error(MG3M_ERR_TOO_LARGE, "D * S above 2^30");
   return MG3M_OK;
 }
 
@@ -194,6 +198,8 @@ int w4(const mg3m_w4* in, void* stream) {
   if (a.M < 1 || a.C < 1 || a.K < 1) return set_error(MG3M_ERR_SHAPE, "M, C and K must be >= 1");
   if (a.group < 32 || a.group % 32 != 0 || a.C % a.group != 0)
     return set_error(MG3M_ERR_SHAPE, "group must be a multiple of 32 that divides C");
+  if (a.M > kMaxSize || a.K > kMaxSize || a.C > kMaxW4Channels)
+    return set_error(MG3M_ERR_TOO_LARGE, "M and K are at most 2^30, C at most 2^20");
   if (a.x == nullptr || a.q == nullptr || a.scale == nullptr || a.y == nullptr)
     return set_error(MG3M_ERR_NULL, "x, q, scale and y must be non-NULL");
   if (reinterpret_cast<uintptr_t>(a.q) % 16 != 0) return set_error(MG3M_ERR_ALIGN, "q must be 16-byte aligned");

@@ -21,6 +21,9 @@ int take_workspace(void* stream, size_t bytes, CallWorkspace* w, std::string* er
 // rc: the status of the launches; returns it, or the error of giving back.
 int give_workspace(void* stream, CallWorkspace* w, int rc, std::string* err);
 
+// Channels of a 4-bit product: its kernels divide by multiplication (matvec_w4.hip).
+constexpr int kMaxW4Channels = 1 << 20;
+
 // Launchers.  Arguments are checked; each returns an mg3m_status.
 int launch_conv1d(const mg3m_conv1d& a, void* stream, std::string* err);        // conv1d.hip
 int launch_conv1d_step(const mg3m_conv1d& a, void* stream, std::string* err);

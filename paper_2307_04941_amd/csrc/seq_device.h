@@ -3,10 +3,10 @@
 
 #include <hip/hip_runtime.h>
 
-#include <algorithm>
 #include <string>
 
 #include "seq.h"
+#include "seq_pieces.h"
 
 namespace mg3m {
 
@@ -39,72 +39,6 @@ inline int launched(const char* what, std::string* err) {
   if (e == hipSuccess) return MG3M_OK;
   *err = std::string(what) + " launch: " + hipGetErrorString(e);
   return MG3M_ERR_HIP;
-}
-
-// The rows of sequence n, inside 0..T whatever begin and end hold.
-struct SeqRange {
-  int b, e;
-};
-__device__ __forceinline__ SeqRange seq_range(const int* begin, const int* end, int n, int N, int T) {
-  if (begin == nullptr) {
-    const int L = T / N;
-    return {n * L, n * L + L};
-  }
-  const int b = min(max(begin[n], 0), T);
-  return {b, min(max(end[n], b), T)};
-}
-
-// Sequences cut into pieces of W tokens, numbered without knowing the lengths
-// on the host: equal sequences have ceil(L / W) pieces each; otherwise the
-// pieces of sequence n are numbered from begin[n] / W + n, which leaves room
-// for them (ceil(len / W) <= end / W - begin / W + 1) and grows with n, so a
-// piece finds its sequence by bisection.  Numbers that no piece has are left
-// out.  W = 0: every sequence is one piece.  Each sequence has at least piece
-// 0, an empty one too.
-struct Piece {
-  int n, k;           // sequence and piece in it; n < 0: none
-  int b, e;           // its rows
-  bool last;          // the sequence's last piece
-};
-inline long long piece_count(const int* begin, int N, int T, int W) {
-  if (W == 0) return N;
-  if (begin == nullptr) return (long long)N * std::max(1, (T / N + W - 1) / W);
-  return (long long)T / W + N;
-}
-__device__ __forceinline__ int piece_base(const int* begin, int n, int T, int W) {
-  return (int)((unsigned)min(max(begin[n], 0), T) / (unsigned)W) + n;
-}
-__device__ __forceinline__ Piece find_piece(const int* begin, const int* end, int N, int T, int W, int id) {
-  Piece p{id, 0, 0, 0, true};
-  if (W != 0) {
-    if (begin == nullptr) {
-      const int per = max(1, (T / N + W - 1) / W);
-      p.n = id / per;
-      p.k = id - p.n * per;
-    } else {
-      int lo = -1, hi = N;            // base(lo) <= id < base(hi)
-      while (hi - lo > 1) {
-        const int mid = (lo + hi) >> 1;
-        if (piece_base(begin, mid, T, W) <= id) lo = mid; else hi = mid;
-      }
-      p.n = lo;
-      if (lo < 0) return p;
-      p.k = id - piece_base(begin, lo, T, W);
-    }
-  }
-  const SeqRange r = seq_range(begin, end, p.n, N, T);
-  const long long b = (long long)r.b + (long long)p.k * W;
-  if (p.k > 0 && b >= r.e) {
-    p.n = -1;
-    return p;
-  }
-  p.b = (int)b;
-  p.e = r.e;
-  if (W != 0 && r.e - p.b > W) {
-    p.e = p.b + W;
-    p.last = false;
-  }
-  return p;
 }
 
 constexpr float kLog2e = 1.44269504088896340736f;

@@ -173,3 +173,25 @@ def test_every_entry_point_is_bound():
     assert len(names) == 6
     for n in names:
         assert getattr(mg3m.load_library(), n).argtypes is not None, n
+
+
+def test_pieces_of_sequences(tmp_path):
+    """tests/seq_pieces.cpp under the address and undefined-behaviour sanitizers."""
+    exe = tmp_path / "pieces"
+    subprocess.run(["g++", "-std=c++17", "-O1", "-g", "-fsanitize=address,undefined", "-fno-sanitize-recover=all",
+                    f"-I{ROOT}/paper_2307_04941_amd/csrc", os.path.join(ROOT, "tests", "seq_pieces.cpp"), "-o", str(exe)],
+                   check=True)
+    run = subprocess.run([str(exe)], capture_output=True, text=True, timeout=300)
+    assert run.returncode == 0 and "pieces ok" in run.stdout, run.stdout + run.stderr
+
+
+@pytest.mark.parametrize("fn,packer,base,change", [
+    ("conv1d_causal_fwd", "_CONV1D", "CONV", dict(T=0x7fff0001, N=1)),
+    ("conv1d_causal_fwd", "_CONV1D", "CONV", dict(C=(1 << 30) + 1, ldx=1 << 30, ldy=1 << 30)),
+    ("selective_scan_fwd", "_SCAN", "SCAN", dict(T=0x7fff0001, N=1)),
+    ("selective_scan_fwd", "_SCAN", "SCAN", dict(D_=(1 << 26) + 64, ldu=1 << 27, lddt=1 << 27, ldz=1 << 27, ldy=1 << 27)),
+    ("matvec_w4_fwd", "_W4", "W4", dict(K=(1 << 30) + 1, ldy=1 << 30)),
+    ("matvec_w4_fwd", "_W4", "W4", dict(M=(1 << 30) + 1)),
+    ("matvec_w4_fwd", "_W4", "W4", dict(C=(1 << 20) + 64, ldx=1 << 21))])
+def test_sizes_past_the_kernels_counters(fn, packer, base, change):
+    assert call(fn, getattr(mg3m, packer), globals()[base], **change) == TOO_LARGE
