@@ -6,6 +6,7 @@
     python experiments.py acc64 [--workloads W,...] [--fixed PLAN;PLAN...] [--reps R] [--out FILE]
     python experiments.py net [--nets vgg16,alexnet,resnet50] [--batch B] [--layout L] [--reps R] [--out FILE]
     python experiments.py datavalues [--workloads W] [--layers L,...] [--reps R] [--rounds N] [--out FILE]
+    python experiments.py sequence [--reps R] [--out FILE]
 
 adaptability -- Sec. 5.1: the channel-scale scenes (5.1.1), the batch sweep
     (5.1.2), the filter-size sweep (5.1.3) and the padding/stride sweep
@@ -35,6 +36,10 @@ datavalues -- the same layers, plans and instruction streams on different
     timed calls per data set and round, in that order).  The MFMA work and the
     cycles it takes do not depend on the values; the power it draws does, and
     with it the clock the chip holds under load.
+sequence -- a state space layer (two projections, causal convolution, selective
+    scan, projection): prompts in fp32 with the 1x1 convolution as projection,
+    single tokens in bf16 with 4-bit weights, the tokens also replayed from a
+    HIP graph.  Per case: time of each operator and of the layer.
 Inputs are the seeded synthetic tensors of ``workloads`` (HWCN, resident on
 the GPU before timing).  Each scene is warmed up for ~100 ms, then timed over
 R calls with HIP events on the calling stream.  One JSON line per scene and
@@ -237,9 +242,101 @@ def _mean(v):
     return round(sum(v) / len(v), 2) if v else None
 
 
+def run_sequence(reps, emit):
+    import torch
+
+    from paper_2307_04941_amd import mg3m
+
+    mg3m.load_library()
+    torch.cuda.set_device(0)
+    taps, S = 4, 16
+
+    def timed(f):
+        for _ in range(3):
+            f()
+        e0, e1 = torch.cuda.Event(enable_timing=True), torch.cuda.Event(enable_timing=True)
+        e0.record()
+        for _ in range(reps):
+            f()
+        e1.record()
+        torch.cuda.synchronize()
+        return round(e0.elapsed_time(e1) * 1e3 / reps, 2)
+
+    def layer(model, width, rows, seqs, token):
+        """The operators of one layer as calls, by name, on buffers of their own."""
+        t = torch.bfloat16 if token else torch.float32
+        g = torch.Generator(device="cuda").manual_seed(1)
+        rank = model // 16
+
+        def normal(*shape, dtype=t, std=1.0):
+            return (torch.randn(*shape, generator=g, device="cuda") * std).to(dtype)
+
+        def project(c, k, x):
+            if not token:
+                w = normal(1, 1, c, k, std=c ** -0.5)
+                y = torch.empty(1, rows, k, 1, device="cuda")
+                image = torch.empty(1, rows, c, 1, device="cuda")
+
+                def call():
+                    image.view(rows, c).copy_(x())
+                    mg3m.conv2d_fwd(image, w, out=y)
+                return call, lambda: y.view(rows, k)
+            q = torch.randint(0, 256, (k, c // 2), generator=g, device="cuda", dtype=torch.int32).to(torch.uint8)
+            s = normal(k, c // 32, std=0.2 * c ** -0.5).abs()
+            y = torch.empty(rows, k, dtype=t, device="cuda")
+            return (lambda: mg3m.matvec_w4(x(), q, s, out=y)), lambda: y
+
+        x = normal(rows, model)
+        call_in, xz = project(model, 2 * width, lambda: x)
+        u, dt, y = (torch.empty(rows, width, dtype=t, device="cuda") for _ in range(3))
+        cs = torch.zeros(seqs, taps - 1, width, dtype=t, device="cuda")
+        hs = torch.zeros(seqs, width, S, device="cuda")
+        w, b = normal(taps, width, std=0.5), normal(width, std=0.1)
+        A = -torch.arange(1, S + 1, device="cuda").repeat(width, 1).float()
+        skip, bias = torch.ones(width, device="cuda"), normal(width, dtype=torch.float32) - 4
+        call_x, dbc = project(width, rank + 2 * S, lambda: u)
+        call_dt, dts = project(rank, width, lambda: dbc()[:, :rank])
+        call_out, _ = project(width, model, lambda: y)
+
+        def shaped(v):
+            return v if token or seqs == 1 else v.unflatten(0, (seqs, rows // seqs))
+
+        def conv():
+            if token:
+                mg3m.conv1d_causal_step(xz()[:, :width], w, cs, b, True, out=u)
+            else:
+                mg3m.conv1d_causal(shaped(xz()[:, :width]), w, b, True, cs, out=shaped(u))
+
+        def scan():
+            B, C, z = dbc()[:, rank:rank + S], dbc()[:, rank + S:], xz()[:, width:]
+            if token:
+                mg3m.selective_scan_step(u, dts(), A, B, C, hs, skip, z, bias, True, out=y)
+            else:
+                mg3m.selective_scan(shaped(u), shaped(dts()), A, shaped(B), shaped(C), skip, shaped(z), bias, True, hs,
+                                    out=shaped(y))
+        return {"in": call_in, "conv": conv, "x": call_x, "dt": call_dt, "scan": scan, "out": call_out}
+
+    for model, width in ((1024, 2048), (2048, 4096)):
+        for rows, seqs, token in ((2048, 1, False), (8192, 4, False), (1, 1, True), (16, 16, True)):
+            ops = layer(model, width, rows, seqs, token)
+
+            def whole():
+                for f in ops.values():
+                    f()
+            rec = {"mode": "sequence", "model": model, "width": width, "states": S, "sequences": seqs, "rows": rows,
+                   "kind": "token" if token else "prompt", "dtype": "bf16, 4-bit weights" if token else "fp32",
+                   "us": {k: timed(f) for k, f in ops.items()}, "layer_us": timed(whole)}
+            if token:
+                graph = torch.cuda.CUDAGraph()
+                with torch.cuda.graph(graph):
+                    whole()
+                rec["layer_graph_us"] = timed(graph.replay)
+            emit(rec)
+
+
 def main():
     ap = argparse.ArgumentParser()
-    ap.add_argument("mode", choices=["adaptability", "ablation", "acc64", "net", "datavalues"])
+    ap.add_argument("mode", choices=["adaptability", "ablation", "acc64", "net", "datavalues", "sequence"])
     ap.add_argument("--layers", default=None, help="datavalues: layer names, comma-separated (default: all)")
     ap.add_argument("--rounds", type=int, default=3, help="datavalues: interleaved rounds")
     ap.add_argument("--nets", default="vgg16,alexnet,resnet50")
@@ -266,6 +363,8 @@ def main():
     if a.mode == "datavalues":
         run_datavalues(a.workloads or "vgg16_n64", a.layers.split(",") if a.layers else None, a.reps, a.rounds,
                        emit)
+    elif a.mode == "sequence":
+        run_sequence(a.reps, emit)
     elif a.mode == "net":
         batch = {k: int(v) for k, v in (kv.split("=") for kv in a.batch.split(","))}
         run_nets(a.nets.split(","), batch, a.layout, a.reps, emit)
