@@ -115,27 +115,60 @@ __global__ __launch_bounds__(256) void conv1d_pieces(ConvArgs a) {
   for (; t < pc.e; ++t) output(t, row(t));
 }
 
+// Single tokens: everything is loaded at once, for what counts is how many
+// loads follow one another.
+template <typename T, int V, int R>
+__global__ __launch_bounds__(256) void conv1d_token(ConvArgs a) {
+  const mg3m_conv1d& p = a.p;
+  const unsigned item = blockIdx.x * 256u + threadIdx.x;
+  if (item >= a.items) return;
+  const int n = item / a.vecs, c = (int)(item - n * (unsigned)a.vecs) * V;
+  using P = Pack<T, V>;
+  T* state = static_cast<T*>(p.state) + (long long)n * (R - 1) * p.C + c;
+  P h[R], w[R], bias{};
+#pragma unroll
+  for (int i = 0; i + 1 < R; ++i) h[i] = *reinterpret_cast<const P*>(state + (long long)i * p.C);
+  h[R - 1] = *reinterpret_cast<const P*>(static_cast<const T*>(p.x) + n * p.ldx + c);
+#pragma unroll
+  for (int i = 0; i < R; ++i) w[i] = *reinterpret_cast<const P*>(static_cast<const T*>(p.w) + (long long)i * p.C + c);
+  if (p.bias != nullptr) bias = *reinterpret_cast<const P*>(static_cast<const T*>(p.bias) + c);
+  P out;
+#pragma unroll
+  for (int k = 0; k < V; ++k) {
+    float s = (float)bias.v[k];
+#pragma unroll
+    for (int i = 0; i < R; ++i) s = fmaf((float)w[i].v[k], (float)h[i].v[k], s);
+    const float act = s * sigmoid(s);
+    out.v[k] = (T)(p.silu ? act : s);
+  }
+#pragma unroll
+  for (int i = 0; i + 1 < R; ++i) *reinterpret_cast<P*>(state + (long long)i * p.C) = h[i + 1];
+  *reinterpret_cast<P*>(static_cast<T*>(p.y) + n * p.ldy + c) = out;
+}
+
+template <typename T, int V, int R>
+void launch_as(const ConvArgs& a, bool token, void* stream) {
+  auto* kernel = token ? conv1d_token<T, V, R> : conv1d_pieces<T, V, R>;
+  kernel<<<(a.items + 255) / 256, 256, 0, static_cast<hipStream_t>(stream)>>>(a);
+}
+
 template <typename T, int V>
-void launch_taps(const ConvArgs& a, void* stream) {
-  const unsigned grid = (a.items + 255) / 256;
-  hipStream_t st = static_cast<hipStream_t>(stream);
+void launch_taps(const ConvArgs& a, bool token, void* stream) {
   switch (a.p.R) {
-    case 1: conv1d_pieces<T, V, 1><<<grid, 256, 0, st>>>(a); break;
-    case 2: conv1d_pieces<T, V, 2><<<grid, 256, 0, st>>>(a); break;
-    case 3: conv1d_pieces<T, V, 3><<<grid, 256, 0, st>>>(a); break;
-    case 4: conv1d_pieces<T, V, 4><<<grid, 256, 0, st>>>(a); break;
-    case 5: conv1d_pieces<T, V, 5><<<grid, 256, 0, st>>>(a); break;
-    case 6: conv1d_pieces<T, V, 6><<<grid, 256, 0, st>>>(a); break;
-    case 7: conv1d_pieces<T, V, 7><<<grid, 256, 0, st>>>(a); break;
-    default: conv1d_pieces<T, V, 8><<<grid, 256, 0, st>>>(a); break;
+    case 1: launch_as<T, V, 1>(a, token, stream); break;
+    case 2: launch_as<T, V, 2>(a, token, stream); break;
+    case 3: launch_as<T, V, 3>(a, token, stream); break;
+    case 4: launch_as<T, V, 4>(a, token, stream); break;
+    case 5: launch_as<T, V, 5>(a, token, stream); break;
+    case 6: launch_as<T, V, 6>(a, token, stream); break;
+    case 7: launch_as<T, V, 7>(a, token, stream); break;
+    default: launch_as<T, V, 8>(a, token, stream); break;
   }
 }
 
 bool aligned16(const void* p) { return reinterpret_cast<uintptr_t>(p) % 16 == 0; }
 
-}  // namespace
-
-int launch_conv1d(const mg3m_conv1d& p, void* stream, std::string* err) {
+int launch(const mg3m_conv1d& p, bool token, void* stream, std::string* err) {
   return with_dtype(p.dtype, [&](auto t) {
     using T = decltype(t);
     constexpr int V = 16 / sizeof(T);
@@ -149,31 +182,32 @@ int launch_conv1d(const mg3m_conv1d& p, void* stream, std::string* err) {
     // first piece may read its state, which the same thread overwrites.
     const int least = p.R - 1 <= kStep ? kStep : 2 * kStep;
     static_assert(2 * kStep >= 7, "R is at most 8");
-    long long items = 0;
-    for (a.W = 32;; a.W /= 2) {
-      items = piece_count(p.begin, p.N, p.T, a.W) * a.vecs;
-      if (a.W == least || items >= 256 * 2048) break;
-    }
-    while (items > 0x7fffffffLL && a.W < (1 << 20)) {
-      a.W *= 2;
-      items = piece_count(p.begin, p.N, p.T, a.W) * a.vecs;
+    long long items = (long long)p.N * a.vecs;
+    if (!token) {
+      for (a.W = 32;; a.W /= 2) {
+        items = piece_count(p.begin, p.N, p.T, a.W) * a.vecs;
+        if (a.W == least || items >= 256 * 2048) break;
+      }
+      while (items > 0x7fffffffLL && a.W < (1 << 20)) {
+        a.W *= 2;
+        items = piece_count(p.begin, p.N, p.T, a.W) * a.vecs;
+      }
     }
     if (items > 0x7fffffffLL) {
       *err = "causal convolution: too many sequences and channels for one launch";
       return (int)MG3M_ERR_TOO_LARGE;
     }
     a.items = (unsigned)items;
-    if (vec) launch_taps<T, V>(a, stream);
-    else launch_taps<T, 1>(a, stream);
+    if (vec) launch_taps<T, V>(a, token, stream);
+    else launch_taps<T, 1>(a, token, stream);
     return launched("causal convolution", err);
   });
 }
 
-int launch_conv1d_step(const mg3m_conv1d& a, void* stream, std::string* err) {
-  mg3m_conv1d s = a;
-  s.T = a.N;
-  s.load_state = 1;
-  return launch_conv1d(s, stream, err);
-}
+}  // namespace
+
+int launch_conv1d(const mg3m_conv1d& p, void* stream, std::string* err) { return launch(p, false, stream, err); }
+
+int launch_conv1d_step(const mg3m_conv1d& p, void* stream, std::string* err) { return launch(p, true, stream, err); }
 
 }  // namespace mg3m
