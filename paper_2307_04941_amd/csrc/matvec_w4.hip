@@ -71,6 +71,14 @@ __device__ __forceinline__ u32x4 expand(unsigned w, unsigned mask, unsigned sixt
   return r;
 }
 
+// Lanes of a wave that exchange values through LDS: the wave's LDS accesses
+// are carried out in order, and the compiler keeps theirs.
+__device__ __forceinline__ void wave_order() {
+  __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
+  __builtin_amdgcn_wave_barrier();
+  __builtin_amdgcn_sched_barrier(0);
+}
+
 __device__ __forceinline__ unsigned pack2(unsigned short lo, unsigned short hi) { return lo | (unsigned)hi << 16; }
 
 // Eight channels of a token as the MFMA takes them, in `parts` registers sets:
@@ -285,11 +293,12 @@ __global__ __launch_bounds__(512) void matvec_w4(W4Args a) {
     for (int i = 0; i < fours; ++i) {
 #pragma unroll
       for (int n = 0; n < 4; ++n) wt[(n * 4 + quarter) * 16 + (col ^ (n * 4 + quarter))] = w[n];
-      __builtin_amdgcn_sched_barrier(0);
+      wave_order();
       load(first(min(i + 1, fours - 1)), w);     // the last one again: not under a condition
       __builtin_amdgcn_sched_barrier(0);
 #pragma unroll
       for (int k = 0; k < 4; k += 2) product(unit0, (i * CW + cw) * 4 + k, k * 4);
+      wave_order();                              // the next four's writes after these reads
     }
   }
 
