@@ -42,9 +42,12 @@
  * override.  HIP launch failures return
  * MG3M_ERR_HIP with the HIP error text in mg3m_last_error(); setting the
  * environment variable MG3M_TEST_FAIL_LAUNCH=1 makes every convolution
- * launch fail that way (nothing is launched), for testing callers' error
+ * launch, and every one of mg3m_seq.h, fail that way (nothing is launched), for testing callers' error
  * paths.  No C++ exception crosses this interface.  Calls on different streams may run
  * concurrently from different host threads.
+ *
+ * mg3m_seq.h has the sequence operators: causal convolution along tokens,
+ * selective scan, products with 4-bit weights.
  *
  * Environment (read at each call that plans a shape):
  *   MG3M_FORCE_PLAN=<override>  applied wherever a call passes no override

@@ -1,6 +1,7 @@
 // C entry points of the sequence operators (include/mg3m_seq.h): validation
 // and dispatch.  Validation finishes before anything is launched.
 #include <cstdint>
+#include <cstdlib>
 #include <exception>
 #include <initializer_list>
 #include <string>
@@ -85,6 +86,13 @@ int check_sequences(const int* begin, const int* end, int T, int N) {
   return MG3M_OK;
 }
 
+// The test hook of conv_launch.hip, for these launches.
+bool launch_failure_injected() {
+  const char* v = std::getenv("MG3M_TEST_FAIL_LAUNCH");
+  return v != nullptr && v[0] == '1' && v[1] == 0;
+}
+int injected() { return set_error(MG3M_ERR_HIP, "kernel launch: failure injected by MG3M_TEST_FAIL_LAUNCH"); }
+
 int element_size(int dtype) { return dtype == MG3M_F32 ? 4 : 2; }
 
 int conv1d(const mg3m_conv1d* in, bool step, void* stream) {
@@ -119,6 +127,7 @@ int conv1d(const mg3m_conv1d* in, bool step, void* stream) {
                            dense("begin", a.begin, a.N, 4),
                            dense("end", a.end, a.N, 4)}))
     return rc;
+  if (launch_failure_injected()) return injected();
   std::string err;
   const int rc = step ? launch_conv1d_step(a, stream, &err) : launch_conv1d(a, stream, &err);
   return rc ? set_error(rc, err) : MG3M_OK;
@@ -175,6 +184,7 @@ int scan(const mg3m_scan* in, bool step, void* stream) {
                            dense("begin", a.begin, a.N, 4),
                            dense("end", a.end, a.N, 4)}))
     return rc;
+  if (launch_failure_injected()) return injected();
   std::string err;
   int rc = MG3M_OK;
   if (step) {
@@ -211,6 +221,7 @@ int w4(const mg3m_w4* in, void* stream) {
                            dense("scale", a.scale, a.K * groups, e),
                            dense("zero", a.zero, a.K * groups, 1)}))
     return rc;
+  if (launch_failure_injected()) return injected();
   std::string err;
   const int rc = launch_w4(a, stream, &err);
   return rc ? set_error(rc, err) : MG3M_OK;

@@ -195,3 +195,13 @@ def test_pieces_of_sequences(tmp_path):
     ("matvec_w4_fwd", "_W4", "W4", dict(C=(1 << 20) + 64, ldx=1 << 21))])
 def test_sizes_past_the_kernels_counters(fn, packer, base, change):
     assert call(fn, getattr(mg3m, packer), globals()[base], **change) == TOO_LARGE
+
+
+@pytest.mark.parametrize("fn,packer,base", [("conv1d_causal_fwd", "_CONV1D", CONV), ("conv1d_causal_step", "_CONV1D", CONV),
+                                            ("selective_scan_fwd", "_SCAN", SCAN), ("selective_scan_step", "_SCAN", SCAN),
+                                            ("matvec_w4_fwd", "_W4", W4)])
+def test_injected_launch_failure(fn, packer, base, monkeypatch):
+    """Valid arguments pass every check and reach the launch, which fails."""
+    monkeypatch.setenv("MG3M_TEST_FAIL_LAUNCH", "1")
+    assert call(fn, getattr(mg3m, packer), base) == HIP
+    assert "MG3M_TEST_FAIL_LAUNCH" in mg3m.mg3m_last_error()
