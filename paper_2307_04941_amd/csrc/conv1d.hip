@@ -53,14 +53,21 @@ __global__ __launch_bounds__(256) void conv1d_pieces(ConvArgs a) {
     for (int k = 0; k < V; ++k) bias[k] = (float)r.v[k];
   }
   // the R - 1 rows before this piece: x's, or at the sequence's start its state's
+  const bool kept = state != nullptr && p.load_state;
+  {
+    // loads without conditions, from rows that are there: all under way at once
+    P r[R];
 #pragma unroll
-  for (int i = 1; i < R; ++i) {
-    const int t = pc.b - R + i;
-    P r{};
-    if (t >= first) r = row(t);
-    else if (state != nullptr && p.load_state) r = *reinterpret_cast<const P*>(state + (long long)(t - first + R - 1) * p.C);
+    for (int i = 1; i < R; ++i) {
+      const int t = pc.b - R + i;
+      const T* at = t >= first ? x + (unsigned long long)(unsigned)t * (unsigned)p.ldx
+                               : kept ? state + (long long)(t - first + R - 1) * p.C : static_cast<const T*>(p.w) + c;
+      r[i] = *reinterpret_cast<const P*>(at);
+    }
 #pragma unroll
-    for (int k = 0; k < V; ++k) h[i][k] = (float)r.v[k];
+    for (int i = 1; i < R; ++i)
+#pragma unroll
+      for (int k = 0; k < V; ++k) h[i][k] = pc.b - R + i >= first || kept ? (float)r[i].v[k] : 0.0f;
   }
   // The thread of the first piece has read the sequence's state, so it writes
   // the one after: rows end - R + 1 .. of state and x together.

@@ -64,17 +64,25 @@ __global__ __launch_bounds__(64 * F) void scan_pieces(ScanArgs a) {
   const int b = __builtin_amdgcn_readfirstlane(pc.b), e = __builtin_amdgcn_readfirstlane(pc.e);
   const int tokens = e - b, tiles = ceil_div(tokens, kTile);
 
-  // states f * P .. + P of channel d
+  // States f * P .. + P of channel d.  Loads without conditions, from elements
+  // that are there, so that they are all under way at once: each under its own
+  // condition, the compiler waits for them one by one.
   float A[P], h[P];
+  const float* start = a.W != 0 ? a.slots : p.load_state ? p.state : p.A;
+  const long long start_at = a.W != 0 ? (long long)id * p.S * p.D + d : p.load_state ? ((long long)n * p.D + d) * p.S : 0;
+  const long long start_step = a.W != 0 ? p.D : p.load_state ? 1 : 0;
+  const bool started = !ENDS && (a.W != 0 || p.load_state);
 #pragma unroll
   for (int i = 0; i < P; ++i) {
-    const int s = f * P + i;
-    A[i] = s < p.S ? p.A[(long long)d * p.S + s] * kLog2e : 0.0f;
-    h[i] = 0.0f;
-    if (!ENDS && s < p.S) {
-      if (a.W != 0) h[i] = a.slots[((long long)id * p.S + s) * p.D + d];
-      else if (p.load_state) h[i] = p.state[((long long)n * p.D + d) * p.S + s];
-    }
+    const int s = min(f * P + i, p.S - 1);
+    A[i] = p.A[(long long)d * p.S + s];
+    h[i] = ENDS ? 0.0f : start[start_at + s * start_step];
+  }
+#pragma unroll
+  for (int i = 0; i < P; ++i) {
+    const bool in = f * P + i < p.S;
+    A[i] = in ? A[i] * kLog2e : 0.0f;
+    h[i] = in && started ? h[i] : 0.0f;
   }
   const float bias = p.dt_bias != nullptr ? p.dt_bias[d] : 0.0f;
   const float skip = !ENDS && p.D_skip != nullptr ? p.D_skip[d] : 0.0f;
