@@ -344,7 +344,7 @@ template <typename T, int RW, int CW>
 int launch_w4_many(W4Args a, void* stream, std::string* err) {
   const mg3m_w4& p = a.p;
   const long long groups = (long long)((p.K + 16 * RW - 1) / (16 * RW)) * ((p.M + 15) / 16);
-  if (groups > 0x7fffffffLL) {
+  if (!fits_launch(groups, 512)) {
     *err = "4-bit product: too many rows for one launch";
     return MG3M_ERR_TOO_LARGE;
   }

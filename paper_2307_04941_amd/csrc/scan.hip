@@ -67,18 +67,19 @@ ScanSpace scan_space(const ScanPlan& s, int T, int D, int G, int S, int N, bool 
 // state behind S stays zero and adds zero.
 template <typename T>
 __global__ __launch_bounds__(256) void scan_pack(ScanArgs a, float* bc, int P, int F) {
-  const long long i = (long long)blockIdx.x * 256 + threadIdx.x;
-  const int w = (int)(i % (2 * P));
-  const long long row = i / (2 * P);
-  const int t = (int)(row % a.p.T);
-  const int gf = (int)(row / a.p.T);
-  if (gf >= a.p.G * F) return;
-  const int g = gf / F, s = (gf - g * F) * P + (w < P ? w : w - P);
-  float v = 0.0f;
-  if (s < a.p.S)
-    v = w < P ? (float)static_cast<const T*>(a.p.B)[t * a.p.ldb + g * a.p.S + s]
-              : (float)static_cast<const T*>(a.p.C)[t * a.p.ldc + g * a.p.S + s];
-  bc[i] = v;
+  const long long all = 2ll * P * a.p.T * a.p.G * F;
+  for (long long i = (long long)blockIdx.x * 256 + threadIdx.x; i < all; i += (long long)gridDim.x * 256) {
+    const int w = (int)(i % (2 * P));
+    const long long row = i / (2 * P);
+    const int t = (int)(row % a.p.T);
+    const int gf = (int)(row / a.p.T);
+    const int g = gf / F, s = (gf - g * F) * P + (w < P ? w : w - P);
+    float v = 0.0f;
+    if (s < a.p.S)
+      v = w < P ? (float)static_cast<const T*>(a.p.B)[t * a.p.ldb + g * a.p.S + s]
+                : (float)static_cast<const T*>(a.p.C)[t * a.p.ldc + g * a.p.S + s];
+    bc[i] = v;
+  }
 }
 
 // The states that a sequence's pieces start from: the first one's is the
@@ -112,7 +113,8 @@ __global__ __launch_bounds__(256) void scan_join(ScanArgs a) {
 #pragma unroll
     for (int j = 0; j < kAt; ++j) {
       if (k0 + j < pieces) slot[(k0 + j) * step] = h;
-      h = fmaf(__builtin_amdgcn_exp2f(A * left[j]), h, end[j]);
+      // nothing stays nothing: a growing piece's factor may pass fp32 where no token's does
+      h = h == 0.0f ? end[j] : fmaf(__builtin_amdgcn_exp2f(A * left[j]), h, end[j]);
     }
   }
 }
@@ -194,9 +196,27 @@ __global__ __launch_bounds__(256) void scan_token(mg3m_scan p, int lanes_log2, i
   }
 }
 
+int token_lanes_log2(int S) {
+  int v = 0;
+  while (4 << v < S) ++v;
+  return v;
+}
+long long token_blocks(const mg3m_scan& p) { return (((long long)p.D << token_lanes_log2(p.S)) + 255) / 256; }
+
+// Work-groups of scan_pieces.
+long long scan_groups(const mg3m_scan& p, const ScanPlan& s) {
+  return piece_count(p.begin, p.N, p.T, s.W) * p.G * ((p.D / p.G + 63) / 64);
+}
+
 bool aligned16(const void* p) { return reinterpret_cast<uintptr_t>(p) % 16 == 0; }
 
 }  // namespace
+
+bool scan_fits(const mg3m_scan& p, bool step) {
+  if (step) return fits_launch(token_blocks(p) * p.N, 256);
+  const ScanPlan s = scan_plan(p.T, p.D, p.G, p.S, p.N, p.begin == nullptr);
+  return fits_launch(scan_groups(p, s), 64 * s.F) && (s.W == 0 || p.N <= 65535);
+}
 
 size_t scan_workspace_bytes(int T, int D, int G, int S, int N) {
   // for equal parts and for given rows, whichever takes more
@@ -220,12 +240,8 @@ int launch_scan(const mg3m_scan& p, void* ws, void* stream, std::string* err) {
   a.sums = reinterpret_cast<float*>(at + m.bc + m.slots);
   a.W = s.W;
   a.blocks = (p.D / p.G + 63) / 64;
-  const long long groups = piece_count(p.begin, p.N, p.T, s.W) * p.G * a.blocks;
-  const long long pack = ((long long)p.G * s.F * p.T * 2 * s.P + 255) / 256;
-  if (groups > 0x7fffffffLL || pack > 0x7fffffffLL || (s.W != 0 && p.N > 65535)) {
-    *err = "selective scan: too many rows, sequences or channels for one launch";
-    return MG3M_ERR_TOO_LARGE;
-  }
+  const long long groups = scan_groups(p, s);
+  const long long pack = std::min(((long long)p.G * s.F * p.T * 2 * s.P + 255) / 256, 1LL << 20);
   const ScanFn ends = kernel_of(p.dtype, s, true), whole = kernel_of(p.dtype, s, false);
   if (ends == nullptr || whole == nullptr) {
     *err = "selective scan: no kernel for this plan";
@@ -246,13 +262,8 @@ int launch_scan(const mg3m_scan& p, void* ws, void* stream, std::string* err) {
 }
 
 int launch_scan_step(const mg3m_scan& p, void* stream, std::string* err) {
-  int lanes_log2 = 0;
-  while (4 << lanes_log2 < p.S) ++lanes_log2;
-  const long long blocks = (((long long)p.D << lanes_log2) + 255) / 256, groups = blocks * p.N;
-  if (groups > 0x7fffffffLL) {
-    *err = "selective scan: too many sequences and channels for one launch";
-    return MG3M_ERR_TOO_LARGE;
-  }
+  const int lanes_log2 = token_lanes_log2(p.S);
+  const long long blocks = token_blocks(p), groups = blocks * p.N;
   const bool vec = p.S % 4 == 0 && aligned16(p.state) && aligned16(p.A);
   return with_dtype(p.dtype, [&](auto t) {
     using T = decltype(t);

@@ -184,6 +184,8 @@ int scan(const mg3m_scan* in, bool step, void* stream) {
                            dense("begin", a.begin, a.N, 4),
                            dense("end", a.end, a.N, 4)}))
     return rc;
+  if (!scan_fits(a, step))
+    return set_error(MG3M_ERR_TOO_LARGE, "selective scan: too many rows, sequences or channels for one launch");
   if (launch_failure_injected()) return injected();
   std::string err;
   int rc = MG3M_OK;

@@ -28,6 +28,7 @@ constexpr int kMaxW4Channels = 1 << 20;
 int launch_conv1d(const mg3m_conv1d& a, void* stream, std::string* err);        // conv1d.hip
 int launch_conv1d_step(const mg3m_conv1d& a, void* stream, std::string* err);
 size_t scan_workspace_bytes(int T, int D, int G, int S, int N);                 // scan.hip
+bool scan_fits(const mg3m_scan& a, bool step);       // whether the launches take this many rows, sequences and channels
 int launch_scan(const mg3m_scan& a, void* ws, void* stream, std::string* err);
 int launch_scan_step(const mg3m_scan& a, void* stream, std::string* err);
 int launch_w4(const mg3m_w4& a, void* stream, std::string* err);                // matvec_w4.hip

@@ -34,6 +34,12 @@ __device__ __forceinline__ float raw_value(unsigned v) {
   }
 }
 
+// Whether a launch takes this many work-groups: grids are counted in threads
+// of 32 bits.
+inline bool fits_launch(long long groups, int threads) {
+  return groups <= 0x7fffffffLL && groups * threads <= 0xffffffffLL;
+}
+
 inline int launched(const char* what, std::string* err) {
   const hipError_t e = hipGetLastError();
   if (e == hipSuccess) return MG3M_OK;

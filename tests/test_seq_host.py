@@ -205,3 +205,14 @@ def test_injected_launch_failure(fn, packer, base, monkeypatch):
     monkeypatch.setenv("MG3M_TEST_FAIL_LAUNCH", "1")
     assert call(fn, getattr(mg3m, packer), base) == HIP
     assert "MG3M_TEST_FAIL_LAUNCH" in mg3m.mg3m_last_error()
+
+
+def test_more_threads_than_a_launch_takes():
+    """Grids are counted in threads of 32 bits: 2^33 are refused."""
+    far = dict(state=at(1000), ldb=16, ldc=16)
+    assert call("selective_scan_step", mg3m._SCAN, SCAN, N=1 << 11, D_=1 << 20, ldu=1 << 20, lddt=1 << 20, ldz=1 << 20,
+                ldy=1 << 20, **far) == TOO_LARGE
+    assert call("selective_scan_fwd", mg3m._SCAN, SCAN, T=1 << 20, N=1 << 20, D_=1024, ldu=1024, lddt=1024, ldz=1024,
+                ldy=1024, state=0, load_state=0) == TOO_LARGE
+    assert call("matvec_w4_fwd", mg3m._W4, W4, M=1 << 16, K=1 << 18, ldy=1 << 18, C=32, group=32, ldx=32,
+                y=at(1000)) == TOO_LARGE

@@ -309,3 +309,18 @@ def test_no_rows_at_all(t):
     assert (st == 1).all()
     mg3m.conv1d_causal(x, torch.ones(4, 24, dtype=tt).cuda(), state=st, offsets=off)
     assert (st == 0).all()
+
+
+def test_growing_states_that_start_at_the_end():
+    """Decays above one, inputs in the last tokens only: a piece's factor
+    passes fp32, the states stay small integers.  exp(4) per token, u = 0 but
+    for the last token, whose state is delta B u exactly."""
+    L, D, S = 4096, 64, 16
+    u = torch.zeros(1, L, D).cuda()
+    u[:, -1] = torch.arange(D).float().cuda() + 1
+    one = torch.ones(1, L, D).cuda()
+    B = torch.ones(1, L, S).cuda()
+    state = torch.zeros(1, D, S).cuda()
+    y = mg3m.selective_scan(u, one, torch.full((D, S), 4.0).cuda(), B, B, state=state)
+    assert torch.equal(state[0], u[0, -1][:, None].expand(D, S))
+    assert torch.equal(y[:, -1], u[:, -1] * S) and not y[:, :-1].any()
