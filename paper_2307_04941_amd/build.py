@@ -1,6 +1,6 @@
 """Build libmg3m.so (the HIP kernels, the planner and the C ABI) for gfx950.
 
-    python -m paper_2307_04941_amd.build                 # libmg3m.so
+    python -m paper_2307_04941_amd.build                 # libmg3m.so, _seq_torch.so
     python -m paper_2307_04941_amd.build --lds-poison    # debug/libmg3m_lds_poison.so
 
 Compiles in-tree with hipcc; the shared library lands next to this file.
@@ -173,6 +173,32 @@ def build(verbose: bool = False, extra=(), lds_poison: bool = False) -> str:
     return lib
 
 
+# csrc/seq_torch.cpp: the sequence operators' binding for ordinary torch
+# tensors, a Python module.  It links torch, not the library, whose entry
+# points mg3m.py hands to it.
+BINDING = os.path.join(PKG, "_seq_torch.so")
+
+
+def build_binding(verbose: bool = False) -> str:
+    """Compile csrc/seq_torch.cpp against the installed torch."""
+    import sysconfig
+
+    import torch
+    home = os.path.dirname(torch.__file__)
+    cmd = ["g++", "-O2", "-std=c++17", "-shared", "-fPIC", "-Wall", "-D__HIP_PLATFORM_AMD__", "-DUSE_ROCM",
+           f"-D_GLIBCXX_USE_CXX11_ABI={int(torch._C._GLIBCXX_USE_CXX11_ABI)}", f"-I{INCLUDE}",
+           f"-isystem{home}/include", f"-isystem{home}/include/torch/csrc/api/include", "-isystem/opt/rocm/include",
+           f"-isystem{sysconfig.get_paths()['include']}", os.path.join(CSRC, "seq_torch.cpp"), "-o", BINDING + ".tmp",
+           f"-L{home}/lib", "-ltorch_python", "-ltorch_cpu", "-lc10", "-lc10_hip"]
+    p = subprocess.run(cmd, capture_output=True, text=True)
+    if p.returncode != 0:
+        raise RuntimeError(f"g++ failed:\n{' '.join(cmd)}\n{p.stdout}\n{p.stderr}")
+    os.replace(BINDING + ".tmp", BINDING)
+    if verbose:
+        print(f"built {BINDING}")
+    return BINDING
+
+
 # tests/c_abi_gpu.c: the C ABI called from plain C (no Python, no torch),
 # linked against the built library; tests/test_c_abi_gpu.py runs it.
 C_ABI_TEST = os.path.join(PKG, "debug", "c_abi_gpu")
@@ -198,3 +224,5 @@ def build_c_abi_test(verbose: bool = False) -> str:
 if __name__ == "__main__":
     args = sys.argv[1:]
     build(verbose=True, extra=[a for a in args if a != "--lds-poison"], lds_poison="--lds-poison" in args)
+    if "--lds-poison" not in args:
+        build_binding(verbose=True)

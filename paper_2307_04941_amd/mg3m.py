@@ -539,12 +539,43 @@ _SCAN = struct.Struct("13PN6q5i3i")
 _W4 = struct.Struct("5P2q6i")
 
 
-# The smallest calls take less time on the device than in this binding, so it
-# looks at each tensor once and builds no torch objects that it can do without
-# (a Stream object, a shape tuple, a device).  torch is imported on first use.
+# The smallest calls take less time on the device than in a binding, so
+# ordinary ones (no stream or workspace given, rows of one or two leading
+# sizes) go through csrc/seq_torch.cpp.  The functions below have the whole
+# contract: what that module does not take, and every refusal, is theirs.
+# torch is imported on first use.
 _torch = None
 _DTYPES = {}
 _raw_stream = None
+_quick = None
+BINDING_PATH = os.path.join(_PKG, "_seq_torch.so")
+
+
+def load_binding():
+    """Load _seq_torch.so (raises if it is not built) and hand it the library's
+    entry points."""
+    global _quick
+    if _quick is None:
+        import importlib.util
+        lib = load_library()
+        if not os.path.exists(BINDING_PATH):
+            raise ImportError(f"{BINDING_PATH} is not built; run `python -m paper_2307_04941_amd.build`")
+        _torch or _seq_torch()
+        spec = importlib.util.spec_from_file_location("_seq_torch", BINDING_PATH)
+        m = importlib.util.module_from_spec(spec)
+        spec.loader.exec_module(m)
+        m.bind(*(ctypes.cast(getattr(lib, f), ctypes.c_void_p).value for f in
+                 ("conv1d_causal_fwd", "conv1d_causal_step", "selective_scan_fwd", "selective_scan_step",
+                  "selective_scan_workspace_bytes", "matvec_w4_fwd")))
+        _quick = m
+    return _quick
+
+
+def _done(y):
+    """What _seq_torch returned: the result, or a status to raise."""
+    if y.__class__ is int:
+        raise Mg3mError(y, mg3m_last_error())
+    return y
 
 
 def _seq_torch():
@@ -557,7 +588,11 @@ def _seq_torch():
     return torch
 
 
-def _seq_call(fn, packed, dev, stream):
+def _seq_call(fn, layout, fields, dev, stream):
+    try:
+        packed = layout.pack(*fields)
+    except struct.error as e:
+        raise ValueError(f"a size does not fit its argument's integer: {e}") from None
     if stream is None:
         stream = _raw_stream(dev)
     elif not isinstance(stream, int):
@@ -667,9 +702,9 @@ def _conv1d(fn, x, w, bias, silu, state, load, dev, dtype, code, T, n, begin, en
     C = shape[-1]
     xp, ldx = _rows_of(x, "x", shape, dtype, dev)
     out, yp, ldy = _out_rows(out, shape, x, dtype, dev)
-    _seq_call(fn, _CONV1D.pack(xp, _dense_of(w, "w", (R, C), dtype, dev), _dense_of(bias, "bias", (C,), dtype, dev),
-                               _dense_of(state, "state", (n, R - 1, C), dtype, dev), yp, begin, end, ldx, ldy, T, C, R,
-                               n, 1 if load else 0, 1 if silu else 0, code, 0), dev, stream)
+    _seq_call(fn, _CONV1D, (xp, _dense_of(w, "w", (R, C), dtype, dev), _dense_of(bias, "bias", (C,), dtype, dev),
+                            _dense_of(state, "state", (n, R - 1, C), dtype, dev), yp, begin, end, ldx, ldy, T, C, R, n,
+                            1 if load else 0, 1 if silu else 0, code, 0), dev, stream)
     return out
 
 
@@ -681,6 +716,10 @@ def conv1d_causal(x, w, bias=None, silu=False, state=None, load_state=False, off
     offsets (N + 1) or begin and end (N each; int32, on the GPU) the rows of N
     sequences.  w: (R, C); bias: (C); state: (N, R - 1, C), written in place
     and with load_state read first.  Returns y, shaped as x."""
+    if stream is None:
+        y = (_quick or load_binding()).conv1d(False, x, w, bias, silu, state, load_state, offsets, begin, end, out)
+        if y is not None:
+            return _done(y)
     dev, dtype, code = _first(x)
     T, n, b, e = _sequences(x, dev, offsets, begin, end)
     return _conv1d("conv1d_causal_fwd", x, w, bias, silu, state, load_state, dev, dtype, code, T, n, b, e, out, stream)
@@ -689,6 +728,10 @@ def conv1d_causal(x, w, bias=None, silu=False, state=None, load_state=False, off
 def conv1d_causal_step(x, w, state, bias=None, silu=False, out=None, stream=None):
     """One token of each of N sequences (conv1d_causal_step): x (N, C), state
     (N, R - 1, C) read and shifted in place (None if R = 1)."""
+    if stream is None:
+        y = (_quick or load_binding()).conv1d(True, x, w, bias, silu, state, True, None, None, None, out)
+        if y is not None:
+            return _done(y)
     dev, dtype, code = _first(x)
     if x.dim() != 2:
         raise ValueError("x is (N, C)")
@@ -714,16 +757,18 @@ def _scan(fn, u, dt, A, B, C, D, z, dt_bias, softplus, state, load, dev, dtype, 
     cp, ldc = _rows_of(C, "C", bshape, dtype, dev, tail)
     zp, ldz = (0, Dn) if z is None else _rows_of(z, "z", shape, dtype, dev)
     wp = wb = 0
+    if workspace is None and stream is None and not fn.endswith("step"):
+        need = selective_scan_workspace_bytes(T, Dn, bshape[-2] if tail == 2 else 1, S, n)
+        workspace = u.new_empty(need, dtype=_torch.uint8) if need else None
     if workspace is not None:
         wp, wb = workspace.data_ptr(), workspace.numel() * workspace.element_size()
         if workspace.get_device() != dev or not workspace.is_contiguous():
             raise ValueError("workspace must be contiguous, on the device of the other tensors")
     out, yp, ldy = _out_rows(out, shape, u, dtype, dev)
-    _seq_call(fn, _SCAN.pack(up, dp, _dense_of(A, "A", (Dn, S), f32, dev), bp, cp, _dense_of(D, "D", (Dn,), f32, dev),
-                             zp, _dense_of(dt_bias, "dt_bias", (Dn,), f32, dev),
-                             _dense_of(state, "state", (n, Dn, S), f32, dev), yp, begin, end, wp, wb, ldu, lddt, ldb,
-                             ldc, ldz, ldy, T, Dn, bshape[-2] if tail == 2 else 1, S, n, 1 if load else 0,
-                             1 if softplus else 0, code), dev, stream)
+    _seq_call(fn, _SCAN, (up, dp, _dense_of(A, "A", (Dn, S), f32, dev), bp, cp, _dense_of(D, "D", (Dn,), f32, dev), zp,
+                          _dense_of(dt_bias, "dt_bias", (Dn,), f32, dev), _dense_of(state, "state", (n, Dn, S), f32, dev),
+                          yp, begin, end, wp, wb, ldu, lddt, ldb, ldc, ldz, ldy, T, Dn,
+                          bshape[-2] if tail == 2 else 1, S, n, 1 if load else 0, 1 if softplus else 0, code), dev, stream)
     return out
 
 
@@ -735,8 +780,14 @@ def selective_scan(u, dt, A, B, C, D=None, z=None, dt_bias=None, softplus=False,
     conv1d_causal.  B, C: rows of (G, S), or of S values for one group.  A:
     (D, S), D and dt_bias: (D), state: (N, D, S), all float32; state is written
     in place and with load_state read first.  workspace: a tensor of at least
-    selective_scan_workspace_bytes(), or None for the library's own.  Returns
-    y, shaped as u."""
+    selective_scan_workspace_bytes(); None: from torch's allocator (in a graph
+    that is being captured, from its pool), or with a stream given the
+    library's own for that stream.  Returns y, shaped as u."""
+    if stream is None and workspace is None:
+        y = (_quick or load_binding()).scan(False, u, dt, A, B, C, D, z, dt_bias, softplus, state, load_state, offsets,
+                                            begin, end, out)
+        if y is not None:
+            return _done(y)
     dev, dtype, code = _first(u)
     T, n, b, e = _sequences(u, dev, offsets, begin, end)
     return _scan("selective_scan_fwd", u, dt, A, B, C, D, z, dt_bias, softplus, state, load_state, dev, dtype, code, T,
@@ -746,6 +797,11 @@ def selective_scan(u, dt, A, B, C, D=None, z=None, dt_bias=None, softplus=False,
 def selective_scan_step(u, dt, A, B, C, state, D=None, z=None, dt_bias=None, softplus=False, out=None, stream=None):
     """One token of each of N sequences (selective_scan_step): u, dt, z (N, D),
     B, C (N, G, S) or (N, S), state (N, D, S) read and updated in place."""
+    if stream is None:
+        y = (_quick or load_binding()).scan(True, u, dt, A, B, C, D, z, dt_bias, softplus, state, True, None, None, None,
+                                            out)
+        if y is not None:
+            return _done(y)
     dev, dtype, code = _first(u)
     if u.dim() != 2:
         raise ValueError("u is (N, D)")
@@ -759,6 +815,10 @@ def matvec_w4(x, q, scale, zero=None, out=None, stream=None):
     (C,), q (K, C / 2) uint8 with the even channel in the low four bits, scale
     (K, C / group) of x's type, zero the same shape in uint8 (None: 8).
     Returns (M, K) or (K,)."""
+    if stream is None:
+        y = (_quick or load_binding()).w4(x, q, scale, zero, out)
+        if y is not None:
+            return _done(y)
     dev, dtype, code = _first(x)
     shape, K, groups, u8 = x.shape, q.shape[0], scale.shape[-1], _torch.uint8
     if len(shape) not in (1, 2):
@@ -768,8 +828,8 @@ def matvec_w4(x, q, scale, zero=None, out=None, stream=None):
         raise ValueError(f"{groups} groups do not divide {C} channels")
     xp, ldx = _rows_of(x, "x", shape, dtype, dev)
     out, yp, ldy = _out_rows(out, (M, K) if len(shape) == 2 else (K,), x, dtype, dev)
-    _seq_call("matvec_w4_fwd", _W4.pack(xp, _dense_of(q, "q", (K, C // 2), u8, dev),
-                                        _dense_of(scale, "scale", (K, groups), dtype, dev),
-                                        _dense_of(zero, "zero", (K, groups), u8, dev), yp, ldx, ldy, M, C, K,
-                                        C // groups, code, 0), dev, stream)
+    _seq_call("matvec_w4_fwd", _W4, (xp, _dense_of(q, "q", (K, C // 2), u8, dev),
+                                     _dense_of(scale, "scale", (K, groups), dtype, dev),
+                                     _dense_of(zero, "zero", (K, groups), u8, dev), yp, ldx, ldy, M, C, K, C // groups,
+                                     code, 0), dev, stream)
     return out

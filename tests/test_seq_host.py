@@ -216,3 +216,16 @@ def test_more_threads_than_a_launch_takes():
                 ldy=1024, state=0, load_state=0) == TOO_LARGE
     assert call("matvec_w4_fwd", mg3m._W4, W4, M=1 << 16, K=1 << 18, ldy=1 << 18, C=32, group=32, ldx=32,
                 y=at(1000)) == TOO_LARGE
+
+
+def test_quick_binding_leaves_the_rest_to_python():
+    """_seq_torch takes ordinary GPU tensors only: for anything else it does nothing and returns None."""
+    quick = mg3m.load_binding()
+    x = torch.zeros(4, 8)
+    assert quick.conv1d(False, x, x, None, True, None, False, None, None, None, None) is None
+    assert quick.conv1d(False, None, x, None, True, None, False, None, None, None, None) is None
+    assert quick.conv1d(False, x) is None and quick.w4() is None
+    assert quick.scan(True, x, x, x, x, x, None, None, None, True, x, True, None, None, None, None) is None
+    assert quick.w4(x, torch.zeros(3, 4, dtype=torch.uint8), x, None, None) is None
+    with pytest.raises(ValueError):
+        quick.bind(1, 2)

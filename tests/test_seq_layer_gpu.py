@@ -324,3 +324,105 @@ def test_growing_states_that_start_at_the_end():
     y = mg3m.selective_scan(u, one, torch.full((D, S), 4.0).cuda(), B, B, state=state)
     assert torch.equal(state[0], u[0, -1][:, None].expand(D, S))
     assert torch.equal(y[:, -1], u[:, -1] * S) and not y[:, :-1].any()
+
+
+# ------------------------------------------------------------ the binding
+@pytest.mark.parametrize("t", T3)
+def test_quick_binding_and_general_one_agree(t):
+    """A given stream takes the general path through the binding: the same
+    results, bit for bit, for dense, strided and three-dimensional rows."""
+    tt, N, L, D, S = ref.TYPES[t], 3, 40, 48, 16
+    g, st, quick = gen(12), torch.cuda.current_stream(), mg3m.load_binding()
+    wide = randn(g, N, L, 2 * D + 5, t=tt).cuda()
+    x, z = wide[..., 3:3 + D], wide[..., 4 + D:4 + 2 * D]
+    w, b = randn(g, 4, D, t=tt).cuda(), randn(g, D, t=tt).cuda()
+    A, B = -torch.rand(D, S, generator=g).cuda(), randn(g, N, L, 2, S, t=tt).cuda()
+    off = torch.tensor([0, 7, 7, N * L], dtype=torch.int32).cuda()
+    q = torch.randint(0, 256, (20, D // 2 + 8), generator=g, dtype=torch.int32).to(torch.uint8).cuda()
+    s = randn(g, 20, 2, t=tt).cuda()
+    xq = randn(g, 5, 70, t=tt).cuda()[:, 2:66]
+    for v in (x, x.contiguous(), x.contiguous().flatten(0, 1), x.flatten(0, 1)):
+        flat = v.dim() == 2
+        zz, BB, o = (z.flatten(0, 1), B.flatten(0, 1), off) if flat else (z, B, None)
+        got = []
+        for kw in ({}, {"stream": st}):
+            cs, hs = torch.ones(N, 3, D, dtype=tt).cuda(), torch.ones(N, D, S).cuda()
+            y = mg3m.conv1d_causal(v, w, b, True, cs, True, offsets=o, **kw)
+            y2 = mg3m.selective_scan(v, y, A, BB, BB, A[:, 0].contiguous(), zz, None, True, hs, True, o, **kw)
+            rows = v if flat else v[:, 0]
+            cs2, hs2 = (u[:1].expand(len(rows), *u.shape[1:]).contiguous() for u in (cs, hs))
+            y3 = mg3m.conv1d_causal_step(rows, w, cs2, b, False, **kw)
+            y4 = mg3m.selective_scan_step(rows, y3, A, BB if flat else BB[:, 0], BB if flat else BB[:, 0], hs2, **kw)
+            got.append((y, y2, cs, hs, y3, y4, cs2, hs2, mg3m.matvec_w4(xq, q, s, **kw)))
+        for a, c in zip(*got):
+            assert torch.equal(a, c)
+    taken = quick.conv1d(False, x, w, b, True, None, False, None, None, None, None)
+    assert taken is not None and torch.equal(taken, mg3m.conv1d_causal(x, w, b, True, stream=st))
+    assert quick.w4(xq, q, s, None, None) is not None
+    out = torch.empty_like(x.contiguous())
+    assert mg3m.conv1d_causal(x, w, b, True, out=out) is out and torch.equal(out, taken)
+
+
+def test_binding_refusals_on_the_gpu():
+    x, w, st = torch.zeros(4, 8).cuda(), torch.zeros(4, 8).cuda(), torch.zeros(4, 3, 8).cuda()
+    with pytest.raises(TypeError):
+        mg3m.conv1d_causal_step(x, w.half(), st)
+    with pytest.raises(ValueError, match="shape"):
+        mg3m.conv1d_causal_step(x, w, st[:3])
+    with pytest.raises(ValueError, match="contiguous"):
+        mg3m.conv1d_causal(x.t(), torch.zeros(4, 4).cuda())
+    with pytest.raises(ValueError):
+        mg3m.conv1d_causal(x, w, offsets=torch.zeros(3, dtype=torch.int32).cuda(), begin=torch.zeros(2).int().cuda())
+    with pytest.raises(mg3m.Mg3mError, match="ALIAS"):
+        mg3m.conv1d_causal(x, w, out=x)
+    with pytest.raises(mg3m.Mg3mError, match="SHAPE"):
+        mg3m.conv1d_causal(x, torch.zeros(9, 8).cuda())
+    with pytest.raises(mg3m.Mg3mError, match="SHAPE"):
+        mg3m.conv1d_causal(x[:1].expand(4, 8), w)
+
+
+def test_graphs_replayed_side_by_side():
+    """Two captured prompts, each with its own workspace, replayed on two
+    streams at once, with eager work between."""
+    cases = [big_case(L=1500), big_case(L=2100, D=192)]
+    wants, graphs, outs, states = [], [], [], []
+    for c in cases:
+        s = torch.zeros_like(c["state"])
+        y = mg3m.selective_scan(c["u"], c["dt"], c["A"], c["B"], c["C"], c["D"], c["z"], c["dt_bias"], True, s)
+        wants.append((y, s))
+        states.append(torch.zeros_like(s))
+    torch.cuda.synchronize()
+    for c, s in zip(cases, states):
+        graph = torch.cuda.CUDAGraph()
+        with torch.cuda.graph(graph):
+            outs.append(mg3m.selective_scan(c["u"], c["dt"], c["A"], c["B"], c["C"], c["D"], c["z"], c["dt_bias"], True, s))
+        graphs.append(graph)
+    streams = [torch.cuda.Stream(), torch.cuda.Stream()]
+    for _ in range(4):
+        for y, s in zip(outs, states):
+            y.zero_()
+            s.zero_()
+        torch.cuda.synchronize()
+        for graph, stream in zip(graphs, streams):
+            with torch.cuda.stream(stream):
+                graph.replay()
+        again = run_big(cases[0], torch.zeros_like(wants[0][1]))
+        torch.cuda.synchronize()
+        for y, s, (want, after) in zip(outs, states, wants):
+            assert torch.equal(y, want) and torch.equal(s, after)
+        assert torch.equal(again, wants[0][0])
+
+
+# --------------------------------------------------- small and growing values
+@pytest.mark.parametrize("M", [1, 2, 5, 16])
+def test_w4_subnormal_tokens(M):
+    """fp16 tokens below the type's normal range count in full."""
+    x = (ints_small(M, 128) * 2.0 ** -22).half()
+    q = torch.randint(0, 256, (40, 64), generator=gen(2), dtype=torch.int32).to(torch.uint8)
+    s = torch.full((40, 2), 1024.0).half()
+    want, _ = ref.w4(x, q, s, None, 64)
+    assert torch.equal(mg3m.matvec_w4(dev(x), dev(q), dev(s)).cpu(), want.half())
+
+
+def ints_small(M, C):
+    return torch.randint(-3, 4, (M, C), generator=gen(M)).float()
