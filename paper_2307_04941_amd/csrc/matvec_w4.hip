@@ -122,7 +122,7 @@ __device__ __forceinline__ void arrange(const T (&v)[8], u32x4 (&out)[W4Type<T>:
   }
 }
 
-// More than four tokens, on the matrix cores.  v_mfma_f32_16x16x32 takes 16
+// More tokens, on the matrix cores.  v_mfma_f32_16x16x32 takes 16
 // tokens (rows) times 16 weight rows (columns); a lane holds eight consecutive
 // channels of a row, which is one dword of weights.
 //
@@ -361,8 +361,8 @@ int launch_w4_many(W4Args a, void* stream, std::string* err) {
   return launched("4-bit product", err);
 }
 
-// Up to four tokens, on the vector ALU: no x in LDS and no barrier, which for
-// few tokens cost more than the products.  A row's blocks of 32 channels (16
+// Few tokens, or few rows, on the vector ALU: no x in LDS and no barrier, which
+// for these cost more than the products.  M tokens to a wave; a row's blocks of 32 channels (16
 // bytes) go to consecutive lanes, so loads are whole cache lines; a lane keeps
 // its channels of the tokens for kRowsPer rows.  16-bit tokens multiply the
 // pairs 16 + q with a two-element dot product (12 instructions for 8 weights
@@ -388,6 +388,8 @@ __global__ __launch_bounds__(256) void matvec_w4_few(W4Args a, int lanes_log2) {
   const int lanes = 1 << lanes_log2;             // on a row
   const int lane = threadIdx.x & (lanes - 1);
   const int row0 = (int)((blockIdx.x * 256u + threadIdx.x) >> lanes_log2) * kRowsPer;
+  const int m0 = blockIdx.y * M, last = p.M - 1 - m0;
+  const T* tokens = static_cast<const T*>(p.x) + m0 * p.ldx;
   const int blocks = p.C / 32, groups = p.C / p.group;
   const unsigned char* zero = p.zero != nullptr ? p.zero : p.q;      // q: read, not used
   unsigned mask = 0x000f000fu << W4Type<T>::kShift, sixteen = W4Type<T>::kSixteen;
@@ -407,7 +409,7 @@ __global__ __launch_bounds__(256) void matvec_w4_few(W4Args a, int lanes_log2) {
     }
 #pragma unroll
     for (int m = 0; m < M; ++m) {
-      const T* x = static_cast<const T*>(p.x) + min(m, p.M - 1) * p.ldx + b * 32;
+      const T* x = tokens + min(m, last) * p.ldx + b * 32;
       T v[32];
       if (a.vec) {
 #pragma unroll
@@ -470,7 +472,7 @@ __global__ __launch_bounds__(256) void matvec_w4_few(W4Args a, int lanes_log2) {
   for (int r = 0; r < kRowsPer; ++r)
 #pragma unroll
     for (int m = 0; m < M; ++m)
-      if (row0 + r < p.K && m < p.M) static_cast<T*>(p.y)[m * p.ldy + row0 + r] = (T)y[r][m];
+      if (row0 + r < p.K && m <= last) static_cast<T*>(p.y)[(m0 + m) * p.ldy + row0 + r] = (T)y[r][m];
 }
 
 template <typename T, int M>
@@ -483,7 +485,8 @@ int launch_w4_few(const W4Args& a, void* stream, std::string* err) {
     *err = "4-bit product: too many rows for one launch";
     return MG3M_ERR_TOO_LARGE;
   }
-  matvec_w4_few<T, M><<<(unsigned)((threads + 255) / 256), 256, 0, static_cast<hipStream_t>(stream)>>>(a, lanes_log2);
+  const dim3 grid((unsigned)((threads + 255) / 256), (unsigned)((p.M + M - 1) / M));
+  matvec_w4_few<T, M><<<grid, 256, 0, static_cast<hipStream_t>(stream)>>>(a, lanes_log2);
   return launched("4-bit product", err);
 }
 
@@ -497,13 +500,17 @@ int launch_w4(const mg3m_w4& p, void* stream, std::string* err) {
     a.vec = reinterpret_cast<uintptr_t>(p.x) % 16 == 0 && (p.ldx * sizeof(T)) % 16 == 0;
     const unsigned blocks = p.group / 32;
     a.per_group = ((1u << 31) + blocks - 1) / blocks;
-    // Tokens by the vector ALU or the matrix cores: 4 of fp16, 8192 to 24576
-    // channels: 47 us against 38, 2 of bf16: 32 against 35; 4 of fp32, 4096 to
-    // 4096: 13 against 17 (three parts each).
+    // Tokens by the vector ALU or the matrix cores: 2 of bf16, 8192 to 24576
+    // channels: 32 us against 35.  More of them while each wave of four rows and
+    // four tokens has a SIMD of its own and rows are long, so that what counts is
+    // how long one takes: 4096 to 1024 channels, 16 tokens of bf16: 7.9 us
+    // against 9.7, of fp32 (three parts): 13 against 22.  Past either: 4096 to
+    // 2048, 16 of bf16: 10.5 against 9.8; 2048 to 1024, 4 of bf16: 5.5 against
+    // 5.2; 512 to 64, 8 of fp32: 7.6 against 6.4.
     if (p.M == 1) return launch_w4_few<T, 1>(a, stream, err);
     if (p.M == 2) return launch_w4_few<T, 2>(a, stream, err);
-    if constexpr (sizeof(T) == 4)
-      if (p.M <= 4) return launch_w4_few<T, 4>(a, stream, err);
+    const long long waves = (long long)((p.K + kRowsPer - 1) / kRowsPer) * ((p.M + 3) / 4);
+    if (waves <= 1024 && p.C * sizeof(T) >= 8192) return launch_w4_few<T, 4>(a, stream, err);
     // Many tiles: four of them share x (64 tokens, 4096 to 4096 channels, bf16:
     // 14 us, two 18); else more waves per row (16 tokens: 16 us, two 11).  LDS
     // does not hold the parts of fp32 tokens for four slices.

@@ -29,7 +29,12 @@ constexpr int pow2_at_least(int v) {
 // nearly all decays twice).  Else sequences are cut into about two pieces per
 // compute unit: not under 32 tokens, where the kernels' start counts, nor over
 // 256, nor into more than 64 pieces, which are joined one after the other (1
-// of 2048, D = 2048: 63 us in pieces of 128, 72 of 64, 280 whole).
+// of 2048, D = 2048: 63 us in pieces of 128, 72 of 64, 280 whole).  Where the
+// host does not know the lengths, the longest sequence may be several times the
+// average, so more sequences and channels are cut (12 to 19 sequences of 470 to
+// 900 on average, 230 to 340 work-groups whole: 140 to 206 us whole, 115 to 142
+// cut; 392 against 158 with 1800 on average; 8 that are equal, 256 work-groups,
+// lose: 99 against 131; and 416: 147 against 170).
 ScanPlan scan_plan(int T, int D, int G, int S, int N, bool equal) {
   const double groups = (double)N * G * ((D / G + 63) / 64);
   // the longest sequence; unknown lengths: four times the average
@@ -37,7 +42,7 @@ ScanPlan scan_plan(int T, int D, int G, int S, int N, bool equal) {
   ScanPlan s{};
   s.P = S <= 16 ? (groups >= 2048 ? 4 : 2) : S <= 32 ? 4 : S <= 128 ? 8 : 16;
   s.F = std::max(2, pow2_at_least((S + s.P - 1) / s.P));
-  if (groups < 224) {
+  if (groups < (equal ? 224 : 352)) {
     s.W = 32;
     while (s.W < 256 && (s.W < longest * groups / 512 || s.W < longest / 64)) s.W *= 2;
     if (s.W >= longest) s.W = 0;

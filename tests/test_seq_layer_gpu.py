@@ -426,3 +426,17 @@ def test_w4_subnormal_tokens(M):
 
 def ints_small(M, C):
     return torch.randint(-3, 4, (M, C), generator=gen(M)).float()
+
+
+@pytest.mark.parametrize("t", T3)
+@pytest.mark.parametrize("M,C,K,group,zero", [(3, 256, 64, 64, True), (4, 2080, 70, 32, False), (13, 4096, 70, 128, True),
+                                              (7, 8192, 33, 32, False), (34, 4096, 50, 4096, True), (3, 1024, 5000, 64, True),
+                                              (6, 2048, 2051, 64, False)])
+def test_w4_few_rows_and_few_tokens(t, M, C, K, group, zero):
+    """Both sides of the rule that picks the vector ALU or the matrix cores, groups of tokens that are not full."""
+    tt = ref.TYPES[t]
+    x, q, s, z = w4_case(tt, M, C, K, group, M + K, zero)
+    want, tol = ref.w4(x, q, s, z, group)
+    near(mg3m.matvec_w4(dev(x), dev(q), dev(s), dev(z)), want, ref.stored(want, tol, tt))
+    x, q, s, z = w4_case(tt, M, C, K, group, M + K, zero, integer=True)
+    assert torch.equal(mg3m.matvec_w4(dev(x), dev(q), dev(s), dev(z)).cpu(), ref.w4(x, q, s, z, group)[0].to(tt))
