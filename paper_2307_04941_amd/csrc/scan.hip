@@ -22,31 +22,35 @@ constexpr int pow2_at_least(int v) {
 // per-channel work best up to S = 16; more states go to more waves, sixteen at
 // most.  Where there are many work-groups anyway, four states per wave cost
 // less in shared work (64 sequences of 512, D = 4096: 545 us against 613; 4 of
-// 4096, D = 4096: 536 against 397).
+// 4096, D = 4096: 536 against 397; cut ones, 1 of 8192, D = 4096: 240 against
+// 252, 1 of 8192, D = 1024: 88 against 81).
 //
 // A work-group walks a whole sequence if that gives nearly every compute unit
 // one (4 of 4096, D = 4096: 397 us whole, 469 cut, though the cut one computes
 // nearly all decays twice).  Else sequences are cut into about two pieces per
 // compute unit: not under 32 tokens, where the kernels' start counts, nor over
-// 256, nor into more than 64 pieces, which are joined one after the other (1
-// of 2048, D = 2048: 63 us in pieces of 128, 72 of 64, 280 whole).  Where the
+// 256, nor into more than 128 pieces, which are joined one after the other (1
+// of 2048, D = 2048: 49 us in pieces of 128, 54 of 64 or of 256, 280 whole; 1 of
+// 8192, D = 64: 35 in pieces of 64, 43 of 32, 39 of 128).  Where the
 // host does not know the lengths, the longest sequence may be several times the
 // average, so more sequences and channels are cut (12 to 19 sequences of 470 to
 // 900 on average, 230 to 340 work-groups whole: 140 to 206 us whole, 115 to 142
 // cut; 392 against 158 with 1800 on average; 8 that are equal, 256 work-groups,
 // lose: 99 against 131; and 416: 147 against 170).
 ScanPlan scan_plan(int T, int D, int G, int S, int N, bool equal) {
-  const double groups = (double)N * G * ((D / G + 63) / 64);
+  const double blocks = (double)G * ((D / G + 63) / 64), groups = N * blocks;
   // the longest sequence; unknown lengths: four times the average
   const double longest = equal ? T / N : std::min<double>(T, 4.0 * T / N + 1);
   ScanPlan s{};
-  s.P = S <= 16 ? (groups >= 2048 ? 4 : 2) : S <= 32 ? 4 : S <= 128 ? 8 : 16;
-  s.F = std::max(2, pow2_at_least((S + s.P - 1) / s.P));
+  double all = groups;                 // work-groups that have something to do
   if (groups < (equal ? 224 : 352)) {
     s.W = 32;
-    while (s.W < 256 && (s.W < longest * groups / 512 || s.W < longest / 64)) s.W *= 2;
+    while (s.W < 256 && (s.W < T * blocks / 600 || s.W < longest / 128)) s.W *= 2;
     if (s.W >= longest) s.W = 0;
+    else all = T * blocks / s.W;
   }
+  s.P = S <= 16 ? (all >= 2048 ? 4 : 2) : S <= 32 ? 4 : S <= 128 ? 8 : 16;
+  s.F = std::max(2, pow2_at_least((S + s.P - 1) / s.P));
   return s;
 }
 
