@@ -132,8 +132,8 @@ __device__ __forceinline__ void arrange(const T (&v)[8], u32x4 (&out)[W4Type<T>:
 // rows at once, they came from one channel of the L2 cache wherever rows are a
 // multiple of 4 KB apart (13 tokens, 8192 to 24576 channels: 54 us).
 //
-// A work-group has eight waves: RW tiles of rows times CW slices of the
-// channels, which are joined through LDS in a fixed order.  It keeps x in LDS
+// A work-group has RW times CW waves: tiles of rows and slices of the channels,
+// which are joined through LDS in a fixed order.  It keeps x in LDS
 // as the MFMA takes it, and the rows' scales, as s and s (16 + zero); long rows
 // in slabs.  fp32 tokens, whose three parts keep the matrix cores busier than
 // the ALU, meet q - zero itself: no second product, and none of the bits that
@@ -141,9 +141,9 @@ __device__ __forceinline__ void arrange(const T (&v)[8], u32x4 (&out)[W4Type<T>:
 // are transposed (lane quarter against dword), after which an MFMA covers 32
 // consecutive channels, which lie in one group.
 template <typename T, int RW, int CW, bool WHOLE>
-__global__ __launch_bounds__(512) void matvec_w4(W4Args a) {
+__global__ __launch_bounds__(64 * RW * CW) void matvec_w4(W4Args a) {
   constexpr int MT = 16;                         // tokens of an MFMA
-  constexpr int kParts = W4Type<T>::kParts, kRows = 16 * RW;
+  constexpr int kParts = W4Type<T>::kParts, kRows = 16 * RW, kWaves = RW * CW, kThreads = 64 * kWaves;
   constexpr bool kExact = kParts == 3;           // q - zero itself
   extern __shared__ u32x4 lds[];
   const mg3m_w4& p = a.p;
@@ -166,7 +166,7 @@ __global__ __launch_bounds__(512) void matvec_w4(W4Args a) {
     x_lane[d] = b * MT + (token ^ b);
   }
   u32x4* wt = lds + wave * 256;                  // [row][16 pieces of 16 bytes]
-  u32x4* xs = lds + 8 * 256;                     // [unit][part][16 blocks of 8 channels][MT]
+  u32x4* xs = lds + kWaves * 256;                     // [unit][part][16 blocks of 8 channels][MT]
   float2* ss = reinterpret_cast<float2*>(xs + (kParts * 16 * MT << a.slab_log2));     // [group][row]
 
   // Four units from channel c0 on: 16 lanes on a row, four rows at a time;
@@ -184,7 +184,7 @@ __global__ __launch_bounds__(512) void matvec_w4(W4Args a) {
 
   // Four loads at a time; those behind the end repeat an element.
   auto stage_scales = [&](int group0, int here) {
-    constexpr int kPer = 512 / kRows;            // threads on a row's scales
+    constexpr int kPer = kThreads / kRows;            // threads on a row's scales
     const int k = threadIdx.x / kPer;
     const long long at = (long long)min(row0 + k, p.K - 1) * groups + group0;
     const unsigned char* zero = p.zero != nullptr ? p.zero : p.q;     // q: read, not used
@@ -206,11 +206,11 @@ __global__ __launch_bounds__(512) void matvec_w4(W4Args a) {
   // Channels behind the last one are zeros, to the slab's end.
   auto stage_x = [&](int unit0, auto vec) {
     const int row_log2 = a.slab_log2 + 4;
-    for (int i0 = threadIdx.x; i0 < tokens << row_log2; i0 += 4 * 512) {
+    for (int i0 = threadIdx.x; i0 < tokens << row_log2; i0 += 4 * kThreads) {
       T v[4][8];
 #pragma unroll
       for (int n = 0; n < 4; ++n) {
-        const int i = i0 + n * 512, b = i & ((1 << row_log2) - 1);
+        const int i = i0 + n * kThreads, b = i & ((1 << row_log2) - 1);
         const int m = min(i >> row_log2, tokens - 1), c = min(unit0 * kUnit + b * 8, p.C - 8);
         const T* x = static_cast<const T*>(p.x) + (m0 + m) * p.ldx + c;
         if constexpr (decltype(vec)::value) {
@@ -224,7 +224,7 @@ __global__ __launch_bounds__(512) void matvec_w4(W4Args a) {
       }
 #pragma unroll
       for (int n = 0; n < 4; ++n) {
-        const int i = i0 + n * 512, m = i >> row_log2, b = i & ((1 << row_log2) - 1);
+        const int i = i0 + n * kThreads, m = i >> row_log2, b = i & ((1 << row_log2) - 1);
         if (m >= tokens) continue;
         u32x4 o[kParts];
         arrange(v[n], o);
@@ -344,11 +344,13 @@ template <typename T, int RW, int CW>
 int launch_w4_many(W4Args a, void* stream, std::string* err) {
   const mg3m_w4& p = a.p;
   const long long groups = (long long)((p.K + 16 * RW - 1) / (16 * RW)) * ((p.M + 15) / 16);
-  if (!fits_launch(groups, 512)) {
+  if (!fits_launch(groups, 64 * RW * CW)) {
     *err = "4-bit product: too many rows for one launch";
     return MG3M_ERR_TOO_LARGE;
   }
-  // LDS: the waves' weights (32 KB), x and scales, all or slabs of up to 48 KB
+  // LDS: the waves' weights (4 KB each), x and scales, all or slabs of up to 48
+  // KB, or what CW slices take at least: 145 KB at most (fp32, groups of 32; 16
+  // bits, 4 tiles of 4 slices, groups of 64)
   const int units = (p.C + kUnit - 1) / kUnit;
   const auto bytes = [&](int log2) {
     return ((size_t)(16 * kUnit * 2 * W4Type<T>::kParts) << log2) +
@@ -357,7 +359,7 @@ int launch_w4_many(W4Args a, void* stream, std::string* err) {
   while (1 << a.slab_log2 < 4 * CW) ++a.slab_log2;
   while (1 << a.slab_log2 < units && bytes(a.slab_log2 + 1) <= 49152) ++a.slab_log2;
   auto* kernel = p.group % kUnit == 0 ? matvec_w4<T, RW, CW, true> : matvec_w4<T, RW, CW, false>;
-  kernel<<<(unsigned)groups, 512, 32768 + bytes(a.slab_log2), static_cast<hipStream_t>(stream)>>>(a);
+  kernel<<<(unsigned)groups, 64 * RW * CW, 4096 * RW * CW + bytes(a.slab_log2), static_cast<hipStream_t>(stream)>>>(a);
   return launched("4-bit product", err);
 }
 
@@ -511,12 +513,26 @@ int launch_w4(const mg3m_w4& p, void* stream, std::string* err) {
     if (p.M == 2) return launch_w4_few<T, 2>(a, stream, err);
     const long long waves = (long long)((p.K + kRowsPer - 1) / kRowsPer) * ((p.M + 3) / 4);
     if (waves <= 1024 && p.C * sizeof(T) >= 8192) return launch_w4_few<T, 4>(a, stream, err);
-    // Many tiles: four of them share x (64 tokens, 4096 to 4096 channels, bf16:
-    // 14 us, two 18); else more waves per row (16 tokens: 16 us, two 11).  LDS
-    // does not hold the parts of fp32 tokens for four slices.
-    const long long tiles = (long long)((p.K + 15) / 16) * ((p.M + 15) / 16);
-    if constexpr (sizeof(T) == 2)
-      if (tiles < 1024) return launch_w4_many<T, 2, 4>(a, stream, err);
+    // One work-group to each of the 256 compute units, with the fewest rows that
+    // do: all of them run the same time and x is staged once per unit (12288
+    // rows of 4096 channels, 13 bf16 tokens: 3 tiles 9.9 us, 2: 17.2; 16384 of
+    // 8192, 16: 4 tiles of four slices 24.0, of two 27.5; 24576, 13: 6 tiles 34,
+    // 4: 39).  Beyond, four tiles, two work-groups to a unit (32768, 16: 42 us,
+    // 6 tiles: 60).  Rows too short for four slices: two (1024 channels, 4096
+    // rows: 5.0 us against 5.7; 1536, 12288: 7.5 against 6.6).  LDS holds neither
+    // the parts of fp32 tokens for four slices or six tiles nor sixteen waves'
+    // weights beside scales of 32.
+    if constexpr (sizeof(T) == 2) {
+      const auto one_each = [&](int rw) {
+        return (long long)((p.K + 16 * rw - 1) / (16 * rw)) * ((p.M + 15) / 16) <= 256;
+      };
+      if (p.C > 11 * kUnit) {
+        if (one_each(2)) return launch_w4_many<T, 2, 4>(a, stream, err);
+        if (one_each(3)) return launch_w4_many<T, 3, 4>(a, stream, err);
+        if (one_each(4) && p.group > 32) return launch_w4_many<T, 4, 4>(a, stream, err);
+        if (!one_each(4) && one_each(6)) return launch_w4_many<T, 6, 2>(a, stream, err);
+      }
+    }
     return launch_w4_many<T, 4, 2>(a, stream, err);
   });
 }

@@ -440,3 +440,16 @@ def test_w4_few_rows_and_few_tokens(t, M, C, K, group, zero):
     near(mg3m.matvec_w4(dev(x), dev(q), dev(s), dev(z)), want, ref.stored(want, tol, tt))
     x, q, s, z = w4_case(tt, M, C, K, group, M + K, zero, integer=True)
     assert torch.equal(mg3m.matvec_w4(dev(x), dev(q), dev(s), dev(z)).cpu(), ref.w4(x, q, s, z, group)[0].to(tt))
+
+
+@pytest.mark.parametrize("t", ["bf16", "f16"])
+@pytest.mark.parametrize("group", [32, 64, 96, 512])
+@pytest.mark.parametrize("M,K", [(5, 8200), (16, 12500), (13, 17001), (9, 25000), (40, 3001)])
+def test_w4_every_tile(t, group, M, K):
+    """Work-groups of two, three, four and six tiles of rows, one to a compute unit, and of four, several."""
+    tt, C = ref.TYPES[t], 1536
+    x, q, s, z = w4_case(tt, M, C, K, group, K, True, integer=True)
+    assert torch.equal(mg3m.matvec_w4(dev(x), dev(q), dev(s), dev(z)).cpu(), ref.w4(x, q, s, z, group)[0].to(tt))
+    x, q, s, z = w4_case(tt, M, C, K, group, K, False)
+    want, tol = ref.w4(x, q, s, z, group)
+    near(mg3m.matvec_w4(dev(x), dev(q), dev(s), dev(z)), want, ref.stored(want, tol, tt))
