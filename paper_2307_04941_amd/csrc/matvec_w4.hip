@@ -348,16 +348,19 @@ int launch_w4_many(W4Args a, void* stream, std::string* err) {
     *err = "4-bit product: too many rows for one launch";
     return MG3M_ERR_TOO_LARGE;
   }
-  // LDS: the waves' weights (4 KB each), x and scales, all or slabs of up to 48
-  // KB, or what CW slices take at least: 145 KB at most (fp32, groups of 32; 16
-  // bits, 4 tiles of 4 slices, groups of 64)
+  // LDS: the waves' weights (4 KB each), x and scales, all or slabs: of up to 48
+  // KB, so that two work-groups fit, or of all there is where one has the unit
+  // (24576 rows of 8192 channels, 13 bf16 tokens: 34 us for 28), and at least
+  // what CW slices take (145 KB at most: 16 bits, 4 tiles of 4 slices, groups of
+  // 64; fp32, groups of 32)
   const int units = (p.C + kUnit - 1) / kUnit;
   const auto bytes = [&](int log2) {
     return ((size_t)(16 * kUnit * 2 * W4Type<T>::kParts) << log2) +
            (((size_t)kUnit << log2) / p.group + 2) * 16 * RW * sizeof(float2);
   };
   while (1 << a.slab_log2 < 4 * CW) ++a.slab_log2;
-  while (1 << a.slab_log2 < units && bytes(a.slab_log2 + 1) <= 49152) ++a.slab_log2;
+  const size_t most = RW * CW > 8 ? 163840 - 4096 * RW * CW : 49152;
+  while (1 << a.slab_log2 < units && bytes(a.slab_log2 + 1) <= most) ++a.slab_log2;
   auto* kernel = p.group % kUnit == 0 ? matvec_w4<T, RW, CW, true> : matvec_w4<T, RW, CW, false>;
   kernel<<<(unsigned)groups, 64 * RW * CW, 4096 * RW * CW + bytes(a.slab_log2), static_cast<hipStream_t>(stream)>>>(a);
   return launched("4-bit product", err);
@@ -516,7 +519,7 @@ int launch_w4(const mg3m_w4& p, void* stream, std::string* err) {
     // One work-group to each of the 256 compute units, with the fewest rows that
     // do: all of them run the same time and x is staged once per unit (12288
     // rows of 4096 channels, 13 bf16 tokens: 3 tiles 9.9 us, 2: 17.2; 16384 of
-    // 8192, 16: 4 tiles of four slices 24.0, of two 27.5; 24576, 13: 6 tiles 34,
+    // 8192, 16: 4 tiles of four slices 24.0, of two 27.5; 24576, 13: 6 tiles 28,
     // 4: 39).  Beyond, four tiles, two work-groups to a unit (32768, 16: 42 us,
     // 6 tiles: 60).  Rows too short for four slices: two (1024 channels, 4096
     // rows: 5.0 us against 5.7; 1536, 12288: 7.5 against 6.6).  LDS holds neither
