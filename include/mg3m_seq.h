@@ -39,7 +39,13 @@
  * other tensor, where rows of one distance that interleave without sharing an
  * element are accepted; MG3M_ERR_TOO_LARGE for T above 2^31 - 2^16, C (of the
  * convolution), M, K or D * S above 2^30, C of the 4-bit product above 2^20, or
- * more work-groups than a launch takes.  Tensors may exceed 4 GiB.
+ * more threads than a launch takes (2^32).  N and M are at least 1, T may be 0.
+ * Tensors may exceed 4 GiB.
+ *
+ * Infinities and NaN in a tensor reach the results that the formulas take them
+ * to, there as either of the two, and no others; rows outside the sequences
+ * may hold them.  Sums of the 4-bit product are of terms up to four times the
+ * formula's, so tokens above 2^120 may overflow.
  */
 #ifndef MG3M_SEQ_H
 #define MG3M_SEQ_H
@@ -95,7 +101,8 @@ int conv1d_causal_step(const mg3m_conv1d *a, void *stream);
  * (in a fixed order: results are the same from run to run).
  * workspace: selective_scan_workspace_bytes() of device memory, 16-byte
  * aligned, or NULL for the one that the library keeps for `stream`
- * (mg3m.h, conv2d_fwd_f32; mg3m_trim_workspace_pool gives it back). */
+ * (mg3m.h, conv2d_fwd_f32; mg3m_trim_workspace_pool gives it back).  Calls in
+ * captured graphs that may run side by side want a workspace each. */
 typedef struct mg3m_scan {
     const void *u, *dt;       /* [T][D], distances ldu, lddt */
     const float *A;           /* [D][S], dense */
@@ -129,9 +136,8 @@ int selective_scan_step(const mg3m_scan *a, void *stream);
  * q: [K][C/2] bytes, the even c in the low four bits, values 0..15 (16-byte
  * aligned); scale: [K][C/group] of the type of x; zero: [K][C/group] bytes,
  * or NULL for 8.  group is a multiple of 32 that divides C.  Made for few
- * tokens: each 16 tokens read the weights once.  A token with an infinity or a
- * NaN gives NaN or infinities in its own row; fp32 channels below 2^-100 lose
- * low bits. */
+ * tokens: each 16 tokens read the weights once.  fp32 channels below 2^-100
+ * lose low bits. */
 typedef struct mg3m_w4 {
     const void *x;            /* [M][C], distance ldx */
     const unsigned char *q;

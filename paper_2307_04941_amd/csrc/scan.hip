@@ -20,10 +20,10 @@ constexpr int pow2_at_least(int v) {
 //
 // Two states per wave and eight waves fill the registers least and share the
 // per-channel work best up to S = 16; more states go to more waves, sixteen at
-// most.  Where there are many work-groups anyway, four states per wave cost
-// less in shared work (64 sequences of 512, D = 4096: 545 us against 613; 4 of
-// 4096, D = 4096: 536 against 397; cut ones, 1 of 8192, D = 4096: 240 against
-// 252, 1 of 8192, D = 1024: 88 against 81).
+// most.  Where there are more than two work-groups to a compute unit anyway,
+// four states per wave cost less in shared work if that leaves four waves (16
+// sequences of 512, S = 16, 256 to 512 work-groups: 59 to 80 us with two states,
+// 71 to 84 with four; 768: 116, 111; 2048: 284, 267; but S = 8, 2048: 200, 239).
 //
 // A work-group walks a whole sequence if that gives nearly every compute unit
 // one (4 of 4096, D = 4096: 397 us whole, 469 cut, though the cut one computes
@@ -49,7 +49,7 @@ ScanPlan scan_plan(int T, int D, int G, int S, int N, bool equal) {
     if (s.W >= longest) s.W = 0;
     else all = T * blocks / s.W;
   }
-  s.P = S <= 16 ? (all >= 2048 ? 4 : 2) : S <= 32 ? 4 : S <= 128 ? 8 : 16;
+  s.P = S <= 8 ? 2 : S <= 16 ? (all > 512 ? 4 : 2) : S <= 32 ? 4 : S <= 128 ? 8 : 16;
   s.F = std::max(2, pow2_at_least((S + s.P - 1) / s.P));
   return s;
 }

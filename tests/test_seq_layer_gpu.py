@@ -453,3 +453,31 @@ def test_w4_every_tile(t, group, M, K):
     x, q, s, z = w4_case(tt, M, C, K, group, K, False)
     want, tol = ref.w4(x, q, s, z, group)
     near(mg3m.matvec_w4(dev(x), dev(q), dev(s), dev(z)), want, ref.stored(want, tol, tt))
+
+
+@pytest.mark.parametrize("t", T3)
+@pytest.mark.parametrize("L,D", [(70, 64), (700, 130)])
+def test_padding_may_hold_anything(t, L, D):
+    """NaN and infinities in the rows of a padded batch that belong to no
+    sequence: results and states as without them, those rows left alone."""
+    tt, N, S = ref.TYPES[t], 3, 16
+    c = {k: dev(v) for k, v in scan_case(tt, N * L, N, D, S, 1, L).items()}
+    w = randn(gen(1), 4, D, t=tt).cuda()
+    begin, length = torch.arange(N) * L, torch.tensor([L - 9, 0, 17])
+    pad = torch.ones(N * L, dtype=torch.bool)
+    for b, n in zip(begin.tolist(), length.tolist()):
+        pad[b:b + n] = False
+    be = [v.int().cuda() for v in (begin, begin + length)]
+    got = []
+    for bad in (0.0, float("nan"), float("inf")):
+        v = {k: c[k].clone() for k in ("u", "dt", "B", "C", "z")}
+        for x in v.values():
+            x[pad.cuda()] = bad
+        hs, cs, out, out2 = c["state"].clone(), torch.ones(N, 3, D, dtype=tt).cuda(), *(torch.full_like(v["u"], 5.0) for _ in "12")
+        mg3m.selective_scan(v["u"], v["dt"], c["A"], v["B"], v["C"], c["D"], v["z"], c["dt_bias"], True, hs, True,
+                            begin=be[0], end=be[1], out=out)
+        mg3m.conv1d_causal(v["u"], w, None, True, cs, True, begin=be[0], end=be[1], out=out2)
+        assert (out[pad.cuda()] == 5).all() and (out2[pad.cuda()] == 5).all()
+        got.append((out, out2, hs, cs))
+    for g in got[1:]:
+        assert all(torch.equal(a, b) for a, b in zip(got[0], g))
