@@ -141,10 +141,15 @@ __device__ __forceinline__ void arrange(const T (&v)[8], u32x4 (&out)[W4Type<T>:
 // are transposed (lane quarter against dword), after which an MFMA covers 32
 // consecutive channels, which lie in one group.
 template <typename T, int RW, int CW, bool WHOLE>
-__global__ __launch_bounds__(64 * RW * CW) void matvec_w4(W4Args a) {
+__global__ __launch_bounds__(64 * RW * CW, sizeof(T) == 2 && RW == 4 ? 4 : 1) void matvec_w4(W4Args a) {
   constexpr int MT = 16;                         // tokens of an MFMA
   constexpr int kParts = W4Type<T>::kParts, kRows = 16 * RW, kWaves = RW * CW, kThreads = 64 * kWaves;
   constexpr bool kExact = kParts == 3;           // q - zero itself
+  // Work-groups with a unit to themselves and registers to spare load x's first
+  // round of a slab (and with eight waves the scales') a slab ahead: 12288 rows of
+  // 8192 channels, 16 bf16 tokens: 21.4 us to 19.2; 8192 rows: 17.5 to 15.5.
+  constexpr bool kAlone = kParts == 1 && RW != 4;
+  constexpr int kAhead = kAlone ? 1 : 0, kScalesAhead = kAlone && kWaves == 8 ? 1 : 0;
   extern __shared__ u32x4 lds[];
   const mg3m_w4& p = a.p;
   const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
@@ -182,57 +187,57 @@ __global__ __launch_bounds__(64 * RW * CW) void matvec_w4(W4Args a) {
     for (int n = 0; n < 4; ++n) w[n] = *reinterpret_cast<const u32x4*>(q + (q_lane[n] + at));
   };
 
-  // Four loads at a time; those behind the end repeat an element.
-  auto stage_scales = [&](int group0, int here) {
-    constexpr int kPer = kThreads / kRows;            // threads on a row's scales
-    const int k = threadIdx.x / kPer;
-    const long long at = (long long)min(row0 + k, p.K - 1) * groups + group0;
-    const unsigned char* zero = p.zero != nullptr ? p.zero : p.q;     // q: read, not used
-    for (int g0 = threadIdx.x % kPer; g0 < here; g0 += 4 * kPer) {
-      float s[4], z[4];
+  // Scales and x go to LDS in rounds of four loads by every thread; those
+  // behind the end repeat an element.
+  constexpr int kPer = kThreads / kRows;         // threads on a row's scales
+  const unsigned char* zero = p.zero != nullptr ? p.zero : p.q;       // q: read, not used
+  const auto load_scales = [&](int group0, int here, int g0, T (&s)[4], unsigned char (&z)[4]) {
+    const long long at = (long long)min(row0 + (int)threadIdx.x / kPer, p.K - 1) * groups + group0;
 #pragma unroll
-      for (int n = 0; n < 4; ++n) {
-        const int g = min(g0 + n * kPer, here - 1);
-        s[n] = (float)static_cast<const T*>(p.scale)[at + g];
-        z[n] = (float)zero[at + g];
-      }
+    for (int n = 0; n < 4; ++n) {
+      const int g = min(g0 + n * kPer, here - 1);
+      s[n] = static_cast<const T*>(p.scale)[at + g];
+      z[n] = zero[at + g];
+    }
+  };
+  const auto put_scales = [&](int here, int g0, const T (&s)[4], const unsigned char (&z)[4]) {
 #pragma unroll
-      for (int n = 0; n < 4; ++n) {
-        const float zr = p.zero != nullptr ? z[n] : 8.0f;
-        if (g0 + n * kPer < here) ss[(g0 + n * kPer) * kRows + k] = float2{s[n], kExact ? zr : s[n] * (16.0f + zr)};
+    for (int n = 0; n < 4; ++n) {
+      const float sr = (float)s[n], zr = p.zero != nullptr ? (float)z[n] : 8.0f;
+      if (g0 + n * kPer < here)
+        ss[(g0 + n * kPer) * kRows + threadIdx.x / kPer] = float2{sr, kExact ? zr : sr * (16.0f + zr)};
+    }
+  };
+  const int row_log2 = a.slab_log2 + 4, items = tokens << row_log2;
+  constexpr int kRaw = sizeof(T) / 2;            // 16 bytes each of eight channels
+  const auto load_x = [&](int unit0, int i0, u32x4 (&v)[4][kRaw]) {
+#pragma unroll
+    for (int n = 0; n < 4; ++n) {
+      const int i = i0 + n * kThreads, b = i & ((1 << row_log2) - 1);
+      const int m = min(i >> row_log2, tokens - 1), c = min(unit0 * kUnit + b * 8, p.C - 8);
+      const T* x = static_cast<const T*>(p.x) + (m0 + m) * p.ldx + c;
+#pragma unroll
+      for (int k = 0; k < kRaw; ++k) {
+        const T* at = x + k * 16 / sizeof(T);
+        if (a.vec) v[n][k] = *reinterpret_cast<const u32x4*>(at);
+        else __builtin_memcpy(&v[n][k], at, 16);
       }
     }
   };
   // Channels behind the last one are zeros, to the slab's end.
-  auto stage_x = [&](int unit0, auto vec) {
-    const int row_log2 = a.slab_log2 + 4;
-    for (int i0 = threadIdx.x; i0 < tokens << row_log2; i0 += 4 * kThreads) {
-      T v[4][8];
+  const auto put_x = [&](int unit0, int i0, const u32x4 (&raw)[4][kRaw]) {
 #pragma unroll
-      for (int n = 0; n < 4; ++n) {
-        const int i = i0 + n * kThreads, b = i & ((1 << row_log2) - 1);
-        const int m = min(i >> row_log2, tokens - 1), c = min(unit0 * kUnit + b * 8, p.C - 8);
-        const T* x = static_cast<const T*>(p.x) + (m0 + m) * p.ldx + c;
-        if constexpr (decltype(vec)::value) {
+    for (int n = 0; n < 4; ++n) {
+      const int i = i0 + n * kThreads, m = i >> row_log2, b = i & ((1 << row_log2) - 1);
+      if (m >= tokens) continue;
+      T v[8];
+      __builtin_memcpy(v, raw[n], sizeof(v));
+      u32x4 o[kParts];
+      arrange(v, o);
+      const bool in = unit0 * kUnit + b * 8 < p.C;
 #pragma unroll
-          for (int k = 0; k < (int)sizeof(T) / 2; ++k)
-            *reinterpret_cast<u32x4*>(v[n] + k * 16 / sizeof(T)) = reinterpret_cast<const u32x4*>(x)[k];
-        } else {
-#pragma unroll
-          for (int k = 0; k < 8; ++k) v[n][k] = x[k];
-        }
-      }
-#pragma unroll
-      for (int n = 0; n < 4; ++n) {
-        const int i = i0 + n * kThreads, m = i >> row_log2, b = i & ((1 << row_log2) - 1);
-        if (m >= tokens) continue;
-        u32x4 o[kParts];
-        arrange(v[n], o);
-        const bool in = unit0 * kUnit + b * 8 < p.C;
-#pragma unroll
-        for (int part = 0; part < kParts; ++part)
-          xs[((b / 16 * kParts + part) * 16 + b % 16) * MT + (m ^ b % 16)] = in ? o[part] : u32x4{};
-      }
+      for (int part = 0; part < kParts; ++part)
+        xs[((b / 16 * kParts + part) * 16 + b % 16) * MT + (m ^ b % 16)] = in ? o[part] : u32x4{};
     }
   };
 
@@ -298,6 +303,15 @@ __global__ __launch_bounds__(64 * RW * CW) void matvec_w4(W4Args a) {
       }
     }
   };
+  u32x4 x_next[4][kRaw];
+  T s_next[4];
+  unsigned char z_next[4];
+  const auto ahead = [&](int unit0) {
+    const int first = a.group_of(unit0 * (kUnit / 32)), end = min(min(unit0 + slab, units) * kUnit, p.C);
+    if (kScalesAhead > 0) load_scales(first, a.group_of(end / 32 - 1) - first + 1, threadIdx.x % kPer, s_next, z_next);
+    load_x(unit0, threadIdx.x, x_next);
+  };
+  if (kAhead > 0) ahead(0);
   for (int unit0 = 0; unit0 < units; unit0 += slab) {
     // this wave's fours of units in the slab: i * CW + cw
     const int fours = (min(slab, units - unit0) + 4 * CW - 1) / (4 * CW);
@@ -306,11 +320,23 @@ __global__ __launch_bounds__(64 * RW * CW) void matvec_w4(W4Args a) {
     load(first(0), w);
     group0 = a.group_of(unit0 * (kUnit / 32));
     const int end = min((min(unit0 + slab, units)) * kUnit, p.C);
+    const int here = a.group_of(end / 32 - 1) - group0 + 1, g0 = threadIdx.x % kPer, t0 = threadIdx.x;
     if (unit0 > 0) __syncthreads();
-    stage_scales(group0, a.group_of(end / 32 - 1) - group0 + 1);
-    if (a.vec) stage_x(unit0, std::true_type{});
-    else stage_x(unit0, std::false_type{});
+    if (kScalesAhead > 0) put_scales(here, g0, s_next, z_next);
+    if (kAhead > 0) put_x(unit0, t0, x_next);
+    for (int g = g0 + kScalesAhead * 4 * kPer; g < here; g += 4 * kPer) {
+      T s[4];
+      unsigned char z[4];
+      load_scales(group0, here, g, s, z);
+      put_scales(here, g, s, z);
+    }
+    for (int i = t0 + kAhead * 4 * kThreads; i < items; i += 4 * kThreads) {
+      u32x4 v[4][kRaw];
+      load_x(unit0, i, v);
+      put_x(unit0, i, v);
+    }
     __syncthreads();
+    if (kAhead > 0 && unit0 + slab < units) ahead(unit0 + slab);
     for (int i = 0; i < fours; ++i) {
 #pragma unroll
       for (int n = 0; n < 4; ++n) wt[(n * 4 + quarter) * 16 + (col ^ (n * 4 + quarter))] = w[n];
@@ -350,7 +376,7 @@ int launch_w4_many(W4Args a, void* stream, std::string* err) {
   }
   // LDS: the waves' weights (4 KB each), x and scales, all or slabs: of up to 48
   // KB, so that two work-groups fit, or of all there is where one has the unit
-  // (24576 rows of 8192 channels, 13 bf16 tokens: 34 us for 28), and at least
+  // (24576 rows of 8192 channels, 13 bf16 tokens: 34 us to 28), and at least
   // what CW slices take (145 KB at most: 16 bits, 4 tiles of 4 slices, groups of
   // 64; fp32, groups of 32)
   const int units = (p.C + kUnit - 1) / kUnit;
@@ -519,7 +545,7 @@ int launch_w4(const mg3m_w4& p, void* stream, std::string* err) {
     // One work-group to each of the 256 compute units, with the fewest rows that
     // do: all of them run the same time and x is staged once per unit (12288
     // rows of 4096 channels, 13 bf16 tokens: 3 tiles 9.9 us, 2: 17.2; 16384 of
-    // 8192, 16: 4 tiles of four slices 24.0, of two 27.5; 24576, 13: 6 tiles 28,
+    // 8192, 16: 4 tiles of four slices 24.0, of two 27.5; 24576, 13: 6 tiles 27,
     // 4: 39).  Beyond, four tiles, two work-groups to a unit (32768, 16: 42 us,
     // 6 tiles: 60).  Rows too short for four slices: two (1024 channels, 4096
     // rows: 5.0 us against 5.7; 1536, 12288: 7.5 against 6.6).  LDS holds neither
