@@ -122,8 +122,12 @@ __global__ __launch_bounds__(256) void scan_join(ScanArgs a) {
 #pragma unroll
     for (int j = 0; j < kAt; ++j) {
       if (k0 + j < pieces) slot[(k0 + j) * step] = h;
-      // nothing stays nothing: a growing piece's factor may pass fp32 where no token's does
-      h = h == 0.0f ? end[j] : fmaf(__builtin_amdgcn_exp2f(A * left[j]), h, end[j]);
+      // A piece's factor may leave fp32's range, at either end, where the state
+      // does not: its whole powers of two are applied by themselves, as many as
+      // lead from any number past any other.  (Factors that are NaN or infinite
+      // by an input reach end[j] as well.)
+      const float x = fminf(fmaxf(A * left[j], -400.0f), 400.0f), whole = rintf(x);
+      h = ldexpf(__builtin_amdgcn_exp2f(x - whole) * h, (int)whole) + end[j];
     }
   }
 }

@@ -1,0 +1,36 @@
+"""The sequence operators (include/mg3m_seq.h) on the GPU where a rule of
+theirs changes sides: states that grow across the pieces of a cut prompt."""
+import pytest
+import torch
+
+import scan_ref
+import seq_ref as ref
+from paper_2307_04941_amd import mg3m
+from test_seq_gpu import dev, near
+
+pytestmark = pytest.mark.gpu
+
+
+# ------------------------------------------------- states that grow or fade
+# A rate, and the state's first value: a piece's factor passes fp32 at its
+# upper end or its lower one, no state does.
+@pytest.mark.parametrize("L,A,h0", [(33, 4.0, 1e-30), (40, 4.0, -1e-34), (63, 2.8, 2.0 ** -140), (33, 5.4, 2.0 ** -140),
+                                    (70, 2.4, 1e-37), (40, -3.2, 1e38)])
+@pytest.mark.parametrize("signed", [False, True])
+def test_states_grow_across_pieces_as_the_formula_says(L, A, h0, signed):
+    """One sequence of few channels is cut at 32 tokens; without inputs its
+    state is h0 exp(A delta t), finite at its end.  signed: rates below zero
+    with negative step sizes, the same."""
+    D, S = 64, 16
+    c = dict(u=torch.zeros(L, D), dt=torch.full((L, D), -1.0 if signed else 1.0),
+             A=torch.full((D, S), -A if signed else A), B=torch.ones(L, 1, S), C=torch.ones(L, 1, S), D=None, z=None,
+             dt_bias=None, state=torch.full((1, D, S), h0))
+    want, after, tol, atol = scan_ref.scan(**c, softplus=False, ranges=[(0, L)], load=True, W=32)
+    assert want.abs().max() < 2.0 ** 127           # the states are of one sign, so no part of y is larger
+    sd = dev(c["state"])
+    y = mg3m.selective_scan(dev(c["u"]), dev(c["dt"]), dev(c["A"]), dev(c["B"]), dev(c["C"]), state=sd, load_state=True)
+    near(sd, after, atol, "state")
+    near(y, want, ref.stored(want, tol, torch.float32), "y")
+    zero = torch.zeros_like(sd)                    # a state of nothing stays nothing
+    y = mg3m.selective_scan(dev(c["u"]), dev(c["dt"]), dev(c["A"]), dev(c["B"]), dev(c["C"]), state=zero, load_state=True)
+    assert not y.any() and not zero.any()
