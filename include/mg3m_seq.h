@@ -44,8 +44,9 @@
  *
  * Infinities and NaN in a tensor reach the results that the formulas take them
  * to, there as either of the two, and no others; rows outside the sequences
- * may hold them.  Sums of the 4-bit product are of terms up to four times the
- * formula's, so tokens above 2^120 may overflow.
+ * may hold them.  Sums of the 4-bit product are formed before the group's scale
+ * and, of 16-bit tokens, with 16 added to q, so tokens or scales above 2^112 may
+ * overflow.
  */
 #ifndef MG3M_SEQ_H
 #define MG3M_SEQ_H

@@ -1,5 +1,6 @@
 """The sequence operators (include/mg3m_seq.h) on the GPU where a rule of
-theirs changes sides: states that grow across the pieces of a cut prompt."""
+theirs changes sides: states that grow across the pieces of a cut
+prompt, weights at their zero point."""
 import pytest
 import torch
 
@@ -34,3 +35,29 @@ def test_states_grow_across_pieces_as_the_formula_says(L, A, h0, signed):
     zero = torch.zeros_like(sd)                    # a state of nothing stays nothing
     y = mg3m.selective_scan(dev(c["u"]), dev(c["dt"]), dev(c["A"]), dev(c["B"]), dev(c["C"]), state=zero, load_state=True)
     assert not y.any() and not zero.any()
+
+
+# ------------------------------------------------- fp32 tokens, 4-bit weights
+@pytest.mark.parametrize("M,C,K", [(1, 4096, 300), (2, 4096, 300), (4, 2048, 40), (16, 4096, 60), (7, 1024, 5000)])
+@pytest.mark.parametrize("group", [32, 128])
+def test_w4_weights_at_their_zero_point_add_nothing(M, C, K, group):
+    """fp32 tokens meet q - zero itself: rows that hold their zero points are
+    zero to the last bit, and with one weight beside them y is its product,
+    which rounds three times."""
+    g = torch.Generator().manual_seed(M + C)
+    x = torch.randn(M, C, generator=g) * 8
+    zero = torch.randint(0, 16, (K, C // group), generator=g).to(torch.uint8)
+    codes = zero.repeat_interleave(group, 1)
+    scale = 0.01 * torch.exp(torch.randn(K, C // group, generator=g))
+    at = torch.arange(K) % C
+    for bump in (0, 1):
+        codes[torch.arange(K), at] ^= bump              # by one, to either side
+        q = codes[:, 0::2] | (codes[:, 1::2] << 4)
+        y = mg3m.matvec_w4(dev(x), dev(q), dev(scale), dev(zero)).cpu()
+        if not bump:
+            assert not y.any()
+            continue
+        rows = torch.arange(K)
+        off = codes[rows, at].double() - zero[rows, at // group].double()
+        want = x.double()[:, at] * (off * scale[rows, at // group].double())
+        near(y, want, want.abs() * 3 * ref.H)
