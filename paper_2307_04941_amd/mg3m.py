@@ -179,6 +179,21 @@ def _stream(stream) -> Optional[int]:
     return stream.cuda_stream
 
 
+def _empty(shape, dtype, device, stream):
+    """A new tensor that a call on `stream` (None: torch's current one) writes.
+    The allocator's blocks belong to the stream they are taken on, whose earlier
+    work may still be under way in them and whose later work may take them
+    over, so a tensor is taken on the stream of its call."""
+    import torch
+    handle = _stream(stream)
+    if stream is None or handle == torch.cuda.current_stream(device).cuda_stream:
+        return torch.empty(shape, dtype=dtype, device=device)
+    if not isinstance(stream, torch.cuda.Stream):
+        stream = torch.cuda.ExternalStream(handle, device=device) if handle else torch.cuda.default_stream(device)
+    with torch.cuda.stream(stream):
+        return torch.empty(shape, dtype=dtype, device=device)
+
+
 def _enc(plan):
     return plan.encode() if isinstance(plan, str) else plan
 
@@ -668,10 +683,10 @@ def _refuse(t, name, shape, dtype, dev):
     raise ValueError(f"{name} has shape {tuple(t.shape)}, expected {tuple(shape)}")
 
 
-def _out_rows(out, shape, like, dtype, dev):
+def _out_rows(out, shape, dtype, dev, stream):
     """(result, its address, its distance between rows)."""
     if out is None:
-        out = like.new_empty(shape)
+        out = _empty(shape, dtype, _torch.device("cuda", dev), stream)
         return out, out.data_ptr(), shape[-1]
     p, ld = _rows_of(out, "out", shape, dtype, dev)
     return out, p, ld
@@ -701,7 +716,7 @@ def _conv1d(fn, x, w, bias, silu, state, load, dev, dtype, code, T, n, begin, en
     shape, R = x.shape, w.shape[0]
     C = shape[-1]
     xp, ldx = _rows_of(x, "x", shape, dtype, dev)
-    out, yp, ldy = _out_rows(out, shape, x, dtype, dev)
+    out, yp, ldy = _out_rows(out, shape, dtype, dev, stream)
     _seq_call(fn, _CONV1D, (xp, _dense_of(w, "w", (R, C), dtype, dev), _dense_of(bias, "bias", (C,), dtype, dev),
                             _dense_of(state, "state", (n, R - 1, C), dtype, dev), yp, begin, end, ldx, ldy, T, C, R, n,
                             1 if load else 0, 1 if silu else 0, code, 0), dev, stream)
@@ -715,7 +730,12 @@ def conv1d_causal(x, w, bias=None, silu=False, state=None, load_state=False, off
     x: (N, L, C) for N equal sequences, or (T, C): one sequence, or with
     offsets (N + 1) or begin and end (N each; int32, on the GPU) the rows of N
     sequences.  w: (R, C); bias: (C); state: (N, R - 1, C), written in place
-    and with load_state read first.  Returns y, shaped as x."""
+    and with load_state read first.  Returns y, shaped as x.
+
+    stream, here and below: a torch stream or a raw handle in place of torch's
+    current one.  The result is then one of that stream's tensors: to be waited
+    for, and record_stream'd, where another one uses it.  The other tensors'
+    work has to be done, or waited for by that stream."""
     if stream is None:
         y = (_quick or load_binding()).conv1d(False, x, w, bias, silu, state, load_state, offsets, begin, end, out)
         if y is not None:
@@ -764,7 +784,7 @@ def _scan(fn, u, dt, A, B, C, D, z, dt_bias, softplus, state, load, dev, dtype, 
         wp, wb = workspace.data_ptr(), workspace.numel() * workspace.element_size()
         if workspace.get_device() != dev or not workspace.is_contiguous():
             raise ValueError("workspace must be contiguous, on the device of the other tensors")
-    out, yp, ldy = _out_rows(out, shape, u, dtype, dev)
+    out, yp, ldy = _out_rows(out, shape, dtype, dev, stream)
     _seq_call(fn, _SCAN, (up, dp, _dense_of(A, "A", (Dn, S), f32, dev), bp, cp, _dense_of(D, "D", (Dn,), f32, dev), zp,
                           _dense_of(dt_bias, "dt_bias", (Dn,), f32, dev), _dense_of(state, "state", (n, Dn, S), f32, dev),
                           yp, begin, end, wp, wb, ldu, lddt, ldb, ldc, ldz, ldy, T, Dn,
@@ -827,7 +847,7 @@ def matvec_w4(x, q, scale, zero=None, out=None, stream=None):
     if groups < 1 or C % groups:
         raise ValueError(f"{groups} groups do not divide {C} channels")
     xp, ldx = _rows_of(x, "x", shape, dtype, dev)
-    out, yp, ldy = _out_rows(out, (M, K) if len(shape) == 2 else (K,), x, dtype, dev)
+    out, yp, ldy = _out_rows(out, (M, K) if len(shape) == 2 else (K,), dtype, dev, stream)
     _seq_call("matvec_w4_fwd", _W4, (xp, _dense_of(q, "q", (K, C // 2), u8, dev),
                                      _dense_of(scale, "scale", (K, groups), dtype, dev),
                                      _dense_of(zero, "zero", (K, groups), u8, dev), yp, ldx, ldy, M, C, K, C // groups,

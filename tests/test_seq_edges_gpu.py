@@ -1,6 +1,6 @@
 """The sequence operators (include/mg3m_seq.h) on the GPU where a rule of
 theirs changes sides: states that grow across the pieces of a cut
-prompt, weights at their zero point."""
+prompt, weights at their zero point, results on a given stream."""
 import pytest
 import torch
 
@@ -61,3 +61,46 @@ def test_w4_weights_at_their_zero_point_add_nothing(M, C, K, group):
         off = codes[rows, at].double() - zero[rows, at // group].double()
         want = x.double()[:, at] * (off * scale[rows, at // group].double())
         near(y, want, want.abs() * 3 * ref.H)
+
+
+# ------------------------------------------------------ results on a stream
+def on_a_stream(call, shape, t, stream):
+    """The result of a call on a stream that is not the current one, which is
+    not to come from a block of the current one's."""
+    free = torch.empty(shape, dtype=t, device="cuda")
+    at = free.data_ptr()
+    del free
+    torch.cuda.synchronize()
+    y = call(stream)
+    torch.cuda.synchronize()
+    again = torch.empty(shape, dtype=t, device="cuda")
+    assert again.data_ptr() == at != y.data_ptr()
+    return y
+
+
+@pytest.mark.parametrize("raw", [False, True])
+@pytest.mark.parametrize("t", ["f32", "bf16"])
+def test_results_come_from_the_given_stream(t, raw):
+    tt, N, C, S = ref.TYPES[t], 40, 192, 16
+    g = torch.Generator().manual_seed(1)
+    rn = lambda *s, t=tt: torch.randn(*s, generator=g).to(t).cuda()  # noqa: E731
+    x, w, B, A = rn(N, C), rn(4, C), rn(N, S), -rn(C, S, t=torch.float32).abs()
+    q, scale = torch.randint(0, 256, (C, C // 2), generator=g).to(torch.uint8).cuda(), rn(C, C // 64)
+    conv_state, state = rn(N, 3, C), rn(N, C, S, t=torch.float32)
+    copies = [(conv_state.clone(), state.clone()) for _ in range(2)]
+    side = torch.cuda.Stream()
+    given = side.cuda_stream if raw else side
+    for f in (lambda st, s: mg3m.conv1d_causal(x, w, silu=True, stream=st),
+              lambda st, s: mg3m.conv1d_causal_step(x, w, s[0], stream=st),
+              lambda st, s: mg3m.selective_scan(x, x, A, B, B, z=x, softplus=True, stream=st),
+              lambda st, s: mg3m.selective_scan_step(x, x, A, B, B, s[1], softplus=True, stream=st),
+              lambda st, s: mg3m.matvec_w4(x, q, scale, stream=st)):
+        want = f(None, copies[0])
+        assert torch.equal(on_a_stream(lambda st: f(st, copies[1]), (N, C), tt, given), want)
+    # raw handles of the current stream, and of the default one while another is current
+    assert torch.equal(mg3m.matvec_w4(x, q, scale, stream=torch.cuda.current_stream().cuda_stream), want)
+    torch.cuda.synchronize()
+    with torch.cuda.stream(side):
+        y = mg3m.matvec_w4(x, q, scale, stream=0)
+    torch.cuda.synchronize()
+    assert torch.equal(y, want)
