@@ -185,8 +185,8 @@ def _empty(shape, dtype, device, stream):
     work may still be under way in them and whose later work may take them
     over, so a tensor is taken on the stream of its call."""
     import torch
-    handle = _stream(stream)
-    if stream is None or handle == torch.cuda.current_stream(device).cuda_stream:
+    handle = None if stream is None or device.type != "cuda" else _stream(stream)
+    if handle is None or handle == torch.cuda.current_stream(device).cuda_stream:
         return torch.empty(shape, dtype=dtype, device=device)
     if not isinstance(stream, torch.cuda.Stream):
         stream = torch.cuda.ExternalStream(handle, device=device) if handle else torch.cuda.default_stream(device)
@@ -273,7 +273,8 @@ def maxpool2d_f32(x, y, N, C, H, W, R, S, stride_h, stride_w, pad_h, pad_w, layo
 
 
 def maxpool2d(x, R, S=None, stride=None, pad=0, layout="HWCN", out=None, stream=None):
-    """Max pooling of a torch tensor on the GPU (allocates y unless `out`)."""
+    """Max pooling of a torch tensor on the GPU (allocates y unless `out`, on
+    the stream of the call)."""
     import torch
     S = R if S is None else S
     sh, sw = _pair(R if stride is None else stride)
@@ -284,7 +285,7 @@ def maxpool2d(x, R, S=None, stride=None, pad=0, layout="HWCN", out=None, stream=
         N, C, H, W = x.shape
     Ho, Wo = maxpool2d_out_dims(H, W, R, S, sh, sw, ph, pw)
     shape = (Ho, Wo, C, N) if _layout(layout) == HWCN else (N, C, Ho, Wo)
-    y = out if out is not None else torch.empty(shape, dtype=torch.float32, device=x.device)
+    y = out if out is not None else _empty(shape, torch.float32, x.device, stream)
     maxpool2d_f32(x, y, N, C, H, W, R, S, sh, sw, ph, pw, layout, stream)
     return y
 
@@ -351,8 +352,7 @@ class Net:
 
     def forward(self, x, out=None, graph=False, stream=None):
         import torch
-        y = out if out is not None else torch.empty(self.shape(self.n_layers), dtype=torch.float32,
-                                                     device=x.device)
+        y = out if out is not None else _empty(self.shape(self.n_layers), torch.float32, x.device, stream)
         fn = load_library().mg3m_net_forward_graph if graph else load_library().mg3m_net_forward
         _check(fn(self._h, _ptr(x), _ptr(y), _stream(stream)))
         return y
@@ -513,7 +513,7 @@ def _pair(v):
 def conv2d_fwd(x, w, stride=1, pad=0, layout="HWCN", plan: Optional[str] = None,
                out=None, workspace=None, stream=None, acc64: bool = False):
     """y = conv(x, w) for torch tensors on the GPU; allocates y unless `out`
-    is given.  stride and pad: an int, or (vertical, horizontal).  With
+    is given, on the stream of the call.  stride and pad: an int, or (vertical, horizontal).  With
     `plan`, `workspace` or unequal per-axis values the _ex / _hw entry
     points are used (workspace allocated here when needed).  acc64=True
     uses conv2d_fwd_f32_acc64 (fp64 accumulation, no workspace)."""
@@ -523,7 +523,7 @@ def conv2d_fwd(x, w, stride=1, pad=0, layout="HWCN", plan: Optional[str] = None,
     ph, pw = _pair(pad)
     Ho, Wo = conv2d_out_dims_hw(H, W, R, S, sh, sw, ph, pw)
     shape = (Ho, Wo, K, N) if _layout(layout) == HWCN else (N, K, Ho, Wo)
-    y = out if out is not None else torch.empty(shape, dtype=torch.float32, device=x.device)
+    y = out if out is not None else _empty(shape, torch.float32, x.device, stream)
     if tuple(y.shape) != shape:
         raise ValueError(f"out has shape {tuple(y.shape)}, expected {shape}")
     if acc64:
@@ -537,7 +537,7 @@ def conv2d_fwd(x, w, stride=1, pad=0, layout="HWCN", plan: Optional[str] = None,
         return y
     wsb = conv2d_fwd_f32_hw_workspace_bytes(N, C, H, W, K, R, S, sh, sw, ph, pw, layout, plan)
     if workspace is None and wsb > 0:
-        workspace = torch.empty((wsb + 3) // 4, dtype=torch.float32, device=x.device)
+        workspace = _empty((wsb + 3) // 4, torch.float32, x.device, stream)
     wsz = workspace.numel() * 4 if workspace is not None else 0
     if square:
         conv2d_fwd_f32_ex(x, w, y, N, C, H, W, K, R, S, sh, ph, layout, workspace, wsz, plan, stream)
