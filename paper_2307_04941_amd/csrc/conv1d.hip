@@ -189,18 +189,23 @@ int launch(const mg3m_conv1d& p, bool token, void* stream, std::string* err) {
     // first piece may read its state, which the same thread overwrites.
     const int least = p.R - 1 <= kStep ? kStep : 2 * kStep;
     static_assert(2 * kStep >= 7, "R is at most 8");
-    long long items = (long long)p.N * a.vecs;
+    long long pieces = p.N, items = pieces * a.vecs;
+    const auto cut = [&] {
+      pieces = piece_count(p.begin, p.N, p.T, a.W);
+      items = pieces * a.vecs;
+    };
+    const auto fits = [&] { return pieces <= 0x7fffffffLL && fits_launch((items + 255) / 256, 256); };
     if (!token) {
       for (a.W = 32;; a.W /= 2) {
-        items = piece_count(p.begin, p.N, p.T, a.W) * a.vecs;
+        cut();
         if (a.W == least || items >= 256 * 2048) break;
       }
-      while (items > 0x7fffffffLL && a.W < (1 << 20)) {
+      while (!fits() && a.W < (1 << 20)) {
         a.W *= 2;
-        items = piece_count(p.begin, p.N, p.T, a.W) * a.vecs;
+        cut();
       }
     }
-    if (items > 0x7fffffffLL) {
+    if (!fits()) {
       *err = "causal convolution: too many sequences and channels for one launch";
       return (int)MG3M_ERR_TOO_LARGE;
     }

@@ -523,12 +523,12 @@ int launch_w4_few(const W4Args& a, void* stream, std::string* err) {
   const mg3m_w4& p = a.p;
   int lanes_log2 = 0;
   while (lanes_log2 < 6 && 32 << lanes_log2 < p.C) ++lanes_log2;
-  const long long threads = (long long)((p.K + kRowsPer - 1) / kRowsPer) << lanes_log2;
-  if (threads > 0x7fffffffLL) {
+  const long long groups = (((long long)((p.K + kRowsPer - 1) / kRowsPer) << lanes_log2) + 255) / 256;
+  if (!fits_launch(groups, 256)) {
     *err = "4-bit product: too many rows for one launch";
     return MG3M_ERR_TOO_LARGE;
   }
-  const dim3 grid((unsigned)((threads + 255) / 256), (unsigned)((p.M + M - 1) / M));
+  const dim3 grid((unsigned)groups, (unsigned)((p.M + M - 1) / M));
   matvec_w4_few<T, M><<<grid, 256, 0, static_cast<hipStream_t>(stream)>>>(a, lanes_log2);
   return launched("4-bit product", err);
 }

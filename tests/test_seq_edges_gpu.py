@@ -1,6 +1,7 @@
 """The sequence operators (include/mg3m_seq.h) on the GPU where a rule of
 theirs changes sides: states that grow across the pieces of a cut
-prompt, weights at their zero point, results on a given stream."""
+prompt, weights at their zero point, results on a given
+stream, launches of many threads."""
 import pytest
 import torch
 
@@ -104,3 +105,47 @@ def test_results_come_from_the_given_stream(t, raw):
         y = mg3m.matvec_w4(x, q, scale, stream=0)
     torch.cuda.synchronize()
     assert torch.equal(y, want)
+
+
+# ------------------------------------------- launches of 2^31 threads and more
+@pytest.fixture
+def large():
+    yield
+    torch.cuda.empty_cache()
+
+
+def test_conv_step_of_2_to_the_31_threads(large):
+    N, C = 65536, 32769                              # odd: a thread per channel
+    x = torch.empty(N, C, device="cuda")
+    x.copy_((torch.arange(N, device="cuda") % 61)[:, None] + torch.arange(C, device="cuda") % 7)
+    w, b = (torch.arange(C, device="cuda") % 5).float()[None], (torch.arange(C, device="cuda") % 3).float()
+    y = mg3m.conv1d_causal_step(x, w, None, b)
+    for i in range(0, N, 4096):
+        assert torch.equal(y[i:i + 4096], x[i:i + 4096] * w + b)
+
+
+def test_conv_of_2_to_the_31_threads(large):
+    """A million sequences, one row among them: the others' states stay."""
+    N, C, n, t = 1 << 20, 2049, 1000003, torch.bfloat16
+    state = torch.empty(N, 1, C, dtype=t, device="cuda")
+    state.copy_((torch.arange(N, device="cuda") % 61)[:, None, None] + torch.arange(C, device="cuda") % 7)
+    before = state.clone()
+    x, w = torch.full((1, C), 3, dtype=t, device="cuda"), torch.full((2, C), 2, dtype=t, device="cuda")
+    offsets = (torch.arange(N + 1, device="cuda") > n).int()
+    y = mg3m.conv1d_causal(x, w, state=state, load_state=True, offsets=offsets)
+    assert torch.equal(y[0], 2 * before[n, 0] + 6)
+    before[n] = 3
+    assert torch.equal(state, before)
+
+
+def test_w4_of_2_to_the_31_threads(large):
+    K, C, t = (1 << 27) + 64, 1056, torch.bfloat16
+    if torch.cuda.mem_get_info()[0] < 120 << 30:
+        pytest.skip("needs 80 GB")
+    x = torch.randint(-3, 4, (1, C), generator=torch.Generator().manual_seed(1)).to(t).cuda()
+    q = torch.full((K, C // 2), 0x98, dtype=torch.uint8, device="cuda")      # 0, 1
+    q[-96:] = 0x7b                                                           # 3, -1
+    scale = torch.ones(K, C // 32, dtype=t, device="cuda")
+    y = mg3m.matvec_w4(x, q, scale)[0].float()
+    even, odd = x[0, 0::2].float().sum(), x[0, 1::2].float().sum()
+    assert (y[:-96] == odd.to(t).float()).all() and (y[-96:] == (3 * even - odd).to(t).float()).all()
