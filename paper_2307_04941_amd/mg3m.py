@@ -761,6 +761,8 @@ def conv1d_causal_step(x, w, state, bias=None, silu=False, out=None, stream=None
 
 def selective_scan_workspace_bytes(T, D, G, S, N) -> int:
     b = ctypes.c_size_t()
+    if not all(-1 << 31 <= v < 1 << 31 for v in (T, D, G, S, N)):       # ctypes would pass the low 32 bits
+        raise ValueError("a size does not fit its argument's integer")
     _check(load_library().selective_scan_workspace_bytes(T, D, G, S, N, ctypes.byref(b)))
     return b.value
 

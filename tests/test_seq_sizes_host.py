@@ -20,3 +20,14 @@ from test_seq_host import CONV, HIP, TOO_LARGE, W4, at, call
 def test_launches_of_up_to_2_to_the_32_threads(fn, packer, base, change, rc):
     far = {k: at(100 * (i + 1)) for i, k in enumerate(base) if base[k] >= at(0) and k not in change}
     assert call(fn, getattr(mg3m, packer), base, **far, **change) == rc
+
+
+@pytest.mark.parametrize("at_", range(5))
+@pytest.mark.parametrize("size", [(1 << 32) + 64, 1 << 31, -(1 << 32) + 64])
+def test_workspace_of_sizes_past_an_int(at_, size):
+    """Not the workspace of the size's low 32 bits."""
+    sizes = [64, 64, 64, 64, 64]
+    assert mg3m.selective_scan_workspace_bytes(*sizes) > 0
+    sizes[at_] = size
+    with pytest.raises(ValueError, match="integer"):
+        mg3m.selective_scan_workspace_bytes(*sizes)
