@@ -11,17 +11,18 @@ FLUSH = 2.0 ** -126          # what a product below fp32's normal range may lose
 
 def scan(u, dt, A, B, C, D, z, dt_bias, softplus, state, ranges, load, W=0):
     """(y, state, bound of y's error before its last rounding, bound of the
-    state's error); rows outside the sequences stay NaN."""
+    state's error), on the tensors' device; rows outside the sequences stay NaN."""
     T, Dn = u.shape
     G, S = B.shape[1:]
     N = len(ranges)
+    on_device = dict(dtype=torch.float64, device=u.device)
     u, dt, A, B, C = (v.double() for v in (u, dt, A, B, C))
-    bias = torch.zeros(Dn, dtype=torch.float64) if dt_bias is None else dt_bias.double()
-    skip = torch.zeros(Dn, dtype=torch.float64) if D is None else D.double()
-    y, tol = torch.full((T, Dn), float("nan"), dtype=torch.float64), torch.zeros(T, Dn, dtype=torch.float64)
-    of = torch.arange(Dn) // (Dn // G)
-    begin, lens = torch.tensor([b for b, _ in ranges]), torch.tensor([max(0, e - b) for b, e in ranges])
-    h = state.double().clone() if load else torch.zeros(N, Dn, S, dtype=torch.float64)
+    bias = torch.zeros(Dn, **on_device) if dt_bias is None else dt_bias.double()
+    skip = torch.zeros(Dn, **on_device) if D is None else D.double()
+    y, tol = torch.full((T, Dn), float("nan"), **on_device), torch.zeros(T, Dn, **on_device)
+    of = torch.arange(Dn, device=u.device) // (Dn // G)
+    begin, lens = (torch.tensor(v, device=u.device) for v in ([b for b, _ in ranges], [max(0, e - b) for b, e in ranges]))
+    h = state.double().clone() if load else torch.zeros(N, Dn, S, **on_device)
     err = torch.zeros_like(h)
     # of the piece so far: the state from nothing and its error, what it started
     # from and that one's error, the exponent of its factor and its error
