@@ -24,19 +24,24 @@ constexpr int pow2_at_least(int v) {
 // four states per wave cost less in shared work if that leaves four waves (16
 // sequences of 512, S = 16, 256 to 512 work-groups: 59 to 80 us with two states,
 // 71 to 84 with four; 768: 116, 111; 2048: 284, 267; but S = 8, 2048: 200, 239).
+// The same holds for pieces (two and four states, S = 16, by work-groups: one
+// sequence of 2000, D = 2048, 500: 49 and 52 us; of 2300, 575: 66, 65; four ragged
+// ones of 2000 together, 500: 52, 53; of 2300, 575: 65, 63), but for few ragged
+// ones in pieces of 256 (2300, D = 4096, 575: 98, 107; 4100, 1025: 145, 151).
 //
 // A work-group walks a whole sequence if that gives nearly every compute unit
 // one (4 of 4096, D = 4096: 397 us whole, 469 cut, though the cut one computes
 // nearly all decays twice).  Else sequences are cut into about two pieces per
 // compute unit: not under 32 tokens, where the kernels' start counts, nor over
-// 256, nor into more than 128 pieces, which are joined one after the other (1
-// of 2048, D = 2048: 49 us in pieces of 128, 54 of 64 or of 256, 280 whole; 1 of
-// 8192, D = 64: 35 in pieces of 64, 43 of 32, 39 of 128).  Where the
-// host does not know the lengths, the longest sequence may be several times the
-// average, so more sequences and channels are cut (12 to 19 sequences of 470 to
-// 900 on average, 230 to 340 work-groups whole: 140 to 206 us whole, 115 to 142
-// cut; 392 against 158 with 1800 on average; 8 that are equal, 256 work-groups,
-// lose: 99 against 131; and 416: 147 against 170).
+// 256, nor, up to 32768 tokens, into more than 128 pieces, which are joined one
+// after the other (1 of 2048, D = 2048: 49 us in pieces of 128, 54 of 64 or of
+// 256, 280 whole; 1 of 8192, D = 64: 35 in pieces of 64, 43 of 32, 39 of 128; 1 of
+// 70000, 274 pieces: 111, 30 of them the join).  Where the host does not know
+// the lengths, the longest sequence may be several times the average, so more
+// sequences and channels are cut (12 to 19 sequences of 470 to 900 on average,
+// 230 to 340 work-groups whole: 140 to 206 us whole, 115 to 142 cut; 392 against
+// 158 with 1800 on average; 8 that are equal, 256 work-groups, lose: 99 against
+// 131; and 416: 147 against 170).
 ScanPlan scan_plan(int T, int D, int G, int S, int N, bool equal) {
   const double blocks = (double)G * ((D / G + 63) / 64), groups = N * blocks;
   // the longest sequence; unknown lengths: four times the average
@@ -243,7 +248,7 @@ bool aligned16(const void* p) { return reinterpret_cast<uintptr_t>(p) % 16 == 0;
 bool scan_fits(const mg3m_scan& p, bool step) {
   if (step) return fits_launch(token_blocks(p) * p.N, 256);
   const ScanPlan s = scan_plan(p.T, p.D, p.G, p.S, p.N, p.begin == nullptr);
-  return fits_launch(scan_groups(p, s), 64 * s.F) && (s.W == 0 || p.N <= 65535);
+  return fits_launch(scan_groups(p, s), 64 * s.F);
 }
 
 size_t scan_workspace_bytes(int T, int D, int G, int S, int N) {
@@ -283,6 +288,7 @@ int launch_scan(const mg3m_scan& p, void* ws, void* stream, std::string* err) {
   }
   if (s.W != 0) {
     ends<<<(unsigned)groups, 64 * s.F, 0, st>>>(a);
+    // N is below 352 here (scan_plan), far below the 65535 of a grid's second dimension
     scan_join<<<dim3((p.D * p.S + 255) / 256, p.N), 256, 0, st>>>(a);
   }
   whole<<<(unsigned)groups, 64 * s.F, 0, st>>>(a);

@@ -268,7 +268,6 @@ ScanFn scan_kernel_of(int P, int F) {
     case 202: return scan_pieces<T, 2, 2, ENDS>;
     case 204: return scan_pieces<T, 2, 4, ENDS>;
     case 208: return scan_pieces<T, 2, 8, ENDS>;
-    case 402: return scan_pieces<T, 4, 2, ENDS>;
     case 404: return scan_pieces<T, 4, 4, ENDS>;
     case 408: return scan_pieces<T, 4, 8, ENDS>;
     case 808: return scan_pieces<T, 8, 8, ENDS>;
