@@ -97,7 +97,9 @@ int conv1d_causal_step(const mg3m_conv1d *a, void *stream);
  *   h[s]  = exp(delta * A[d][s]) * h[s] + delta * B[t][g][s] * u[t][d]
  *   y     = sum_s C[t][g][s] * h[s] + D[d] * u[t][d]
  *   y[t][d] = z ? y * z[t][d] * sigmoid(z[t][d]) : y
- * S is 1..256, G divides D.  Long prompts of few channels are cut along the
+ * S is 1..256, G divides D.  exp of a token's delta * A is an fp32 number:
+ * infinite for exponents above 88, where states grow, and zero below -87; rates
+ * are below 2^127 in size, or infinite.  Long prompts of few channels are cut along the
  * tokens: the pieces run side by side and are joined through their end states
  * (in a fixed order: results are the same from run to run).
  * workspace: selective_scan_workspace_bytes() of device memory, 16-byte
